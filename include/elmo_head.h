@@ -33,7 +33,8 @@ typedef struct elmo_head elmo_head_t; /* opaque, host-side */
 
 /* Storage format of the classifier weights (Section 4.1 pure 16-bit; Section 4.3 8-bit).
  * ELMO_FP8_E4M3 is the OCP "FN" flavour: bias 7, largest finite value 448, no infinities. */
-enum { ELMO_BF16 = 0, ELMO_FP8_E4M3 = 1, ELMO_FP32 = 2 /* optimiser moments of elmo_kahan_adamw only */ };
+enum { ELMO_BF16 = 0, ELMO_FP8_E4M3 = 1, ELMO_FP32 = 2 /* optimiser moments of elmo_kahan_adamw, values of the row-wise operators */,
+       ELMO_INT8 = 3 /* 8-bit rows of elmo_rms_norm */ };
 
 /* ELMO_SR: the update rounds with stochastic rounding (Eq. 1), otherwise to nearest even.
  * ELMO_KAHAN: a BF16 compensation buffer carries the rounding error of every update into the
@@ -208,6 +209,84 @@ uint32_t elmo_dropout_keep16(uint64_t seed, uint64_t step, uint64_t block, uint3
 
 /* Host-side Philox4x32-10 (Salmon et al., SC'11) as used for the rounding fields. */
 void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t out[4]);
+
+/* ---------------------------------------------------------------------------------------------
+ * The output end of a language model: norm, 8-bit integer product, sampling, distillation.
+ *
+ * Rules of these calls, beside the general ones:
+ *  - Matrices are row-major with elements of a row next to each other; *_stride is the number of
+ *    elements from one row to the next, at least the row's length (any value for a single row).
+ *    Rows need no alignment beyond their elements'.  Nothing between rows is written.
+ *  - Values are ELMO_BF16 or ELMO_FP32 as the dtype argument says; sums are FP32 or wider, every
+ *    output is rounded once, to nearest even (overflow to infinity, NaN kept).
+ *  - A call with no rows is a no-op.  Workspaces are scratch of the call: two calls that may
+ *    overlap in time (streams, captured graphs) need one each.
+ *  - Only kernels are enqueued: calls can be captured into a HIP graph.  The same call gives the
+ *    same bits every time.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of rows of d elements (1 <= d <= 65536), behind a residual's addition:
+ *   h = x + residual (x alone if residual is NULL),  y = weight * h / sqrt(mean(h^2) + eps)
+ * weight [d] (NULL = ones) has a dtype of its own.  sum_out (NULL = not wanted; needs a residual)
+ * receives h rounded to dtype, y is formed from the unrounded h.  y_dtype: ELMO_BF16 or ELMO_FP32, or 8 bits
+ * with a scale per row in scale_out [rows]: with p = weight * h and m = max |p| of the row
+ *   ELMO_INT8:      y = round(127 p / m),       scale = m / (127 sqrt(mean(h^2) + eps))
+ *   ELMO_FP8_E4M3:  y = round_E4M3(448 p / m),  scale = m / (448 sqrt(mean(h^2) + eps))
+ * so that y * scale is the norm; the quotient is p * (127 * (1 / m)), p exact and three FP64 roundings.  A row of zeros gives zeros and scale 0; a row that holds an infinity or NaN, or squares beyond FP32,
+ * gives zeros and scale NaN.  sum_out may be x or residual, y may be x or sum_out's place, where address, stride and dtype are the same. */
+int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int64_t d, const void* residual,
+                  int64_t residual_stride, const void* weight, int weight_dtype, float eps, void* sum_out,
+                  int64_t sum_stride, void* y, int64_t y_stride, int y_dtype, float* scale_out, void* hip_stream);
+
+/* Its backward pass.  h: what was normalised (sum_out, or x without a residual).  With R = 1 / sqrt(mean(h^2) + eps), g = weight * dy:
+ *   dh = R (g - h R^2 mean(g h)) + dsum      (the gradient of x and of the residual alike)
+ *   dweight[j] = sum over rows of R dy h     (FP32 [d], overwritten; NULL = not wanted; zeros for no rows)
+ * dsum (NULL = none) is the gradient that reaches sum_out from elsewhere.  dh may be dy, h or dsum where address and stride are
+ * the same.  dweight needs a workspace of elmo_rms_norm_backward_bytes(rows, d) bytes, 4-byte aligned. */
+size_t elmo_rms_norm_backward_bytes(int64_t rows, int64_t d);
+int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int64_t h_stride, int dtype, int64_t rows,
+                           int64_t d, const void* weight, int weight_dtype, float eps, const void* dsum,
+                           int64_t dsum_stride, void* dh, int64_t dh_stride, float* dweight, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
+
+/* 8-bit integer product with a scale for each row of either operand (token and output channel):
+ *   out[m, n] = (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]
+ * a [M, K] and b [N, K] int8 (all 256 values), scales and bias FP32 (bias NULL = none), out [M, N] in out_dtype.  The sum is exact
+ * (0 <= K <= 131071; of no products it is 0).  M and N up to 2^30. */
+int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, const int8_t* b, int64_t b_stride,
+                     const float* b_scale, const float* bias, int64_t M, int64_t N, int64_t K, void* out,
+                     int64_t out_stride, int out_dtype, void* hip_stream);
+
+/* One token for each row of V logits (1 <= V < 2^31), from a given random number u[row] in [0, 1).  Tokens are ordered by (logit
+ * falling, index rising) and weigh exp((z - max z) / temperature).  Kept are the first top_k of them, of those the shortest beginning
+ * that has at least top_p of their weight, and of those the ones of weight >= min_p (relative to the largest).  The token is the
+ * first one in order of index at which the kept weight so far exceeds u times the kept weight.
+ * temperature, top_k, top_p, min_p: one value a row, or NULL (1, off, off, off).  temperature <= 0 or NaN: the largest logit, lowest
+ * index.  top_k < 1, top_p >= 1 or NaN, min_p <= 0 or NaN: off; top_p <= 0 keeps one token, min_p >= 1 those equal to the largest.  u is
+ * clamped to [0, 1), NaN counts as 0.  Logits of -infinity and NaN are never drawn; beside logits of +infinity nothing else is.
+ * Weights are whole multiples of 2^-F of the largest, F = min(50, 62 - ceil(log2 V)), computed in FP64 (a token below half of that
+ * is never drawn), and their sums are exact: the token does not depend on how a row is split.
+ * idx_out [rows]: the token, -1 where a row has none; prob_out [rows] (NULL = not wanted): its share of the kept weight, 0 where there
+ * is none.  workspace: elmo_sample_bytes(rows, V) bytes, 256-byte aligned (NULL if that is 0). */
+size_t elmo_sample_bytes(int64_t rows, int64_t V);
+int elmo_sample(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const float* u,
+                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* idx_out,
+                float* prob_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits, loss and gradient in one call.  teacher_idx, teacher_logits [rows, K], dense: the
+ * teacher's tokens and their logits, 1 <= K <= 1024; entries whose index is outside [0, V) do not count, an index that appears
+ * twice counts twice.  With q = softmax(teacher / T) over the row's entries, p = softmax(logits / T) over all V (1 <= V < 2^31),
+ * T = temperature in [1e-6, 1e6], v = row_weight[row] (NULL = 1):
+ *   loss_out[row] = v T^2 sum_j q_j log(q_j / p_j)       grad_out = d loss / d logits = v T (p - q)
+ * grad_out (NULL = not wanted) has the logits' dtype and may be the logits themselves where the strides are the same.  Rows of weight
+ * 0 and rows without a teacher entry above -infinity give loss 0 and a gradient of zeros whatever the logits hold.  A logit of -infinity has p = 0 (loss
+ * +infinity if q > 0 there; so for a row of nothing else); NaN and +infinity make the row's loss and gradient NaN.
+ * workspace: elmo_distill_bytes(rows, V) bytes, 256-byte aligned (NULL if that is 0). */
+size_t elmo_distill_bytes(int64_t rows, int64_t V);
+int elmo_distill(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V,
+                 const int32_t* teacher_idx, const void* teacher_logits, int teacher_dtype, int64_t K, float temperature,
+                 const float* row_weight, float* loss_out, void* grad_out, int64_t grad_stride, void* workspace,
+                 size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,7 @@ from .build import LIB_PATH
 ELMO_BF16 = 0
 ELMO_FP8_E4M3 = 1
 ELMO_FP32 = 2
+ELMO_INT8 = 3
 ELMO_SR = 1
 ELMO_KAHAN = 2
 ELMO_VALIDATE = 4
@@ -84,11 +85,30 @@ _lib.elmo_kahan_adamw.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p
                                   C.c_double, C.c_double, C.c_float, C.c_float, C.c_int64, C.c_void_p]
 _lib.elmo_dropout_keep16.restype = C.c_uint32
 _lib.elmo_dropout_keep16.argtypes = [C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint32]
+_I, _L, _F, _P, _Z = C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_size_t
+_lib.elmo_rms_norm.restype = _I
+_lib.elmo_rms_norm.argtypes = [_P, _L, _I, _L, _L, _P, _L, _P, _I, _F, _P, _L, _P, _L, _I, _P, _P]
+_lib.elmo_rms_norm_backward_bytes.restype = _Z
+_lib.elmo_rms_norm_backward_bytes.argtypes = [_L, _L]
+_lib.elmo_rms_norm_backward.restype = _I
+_lib.elmo_rms_norm_backward.argtypes = [_P, _L, _P, _L, _I, _L, _L, _P, _I, _F, _P, _L, _P, _L, _P, _P, _Z, _P]
+_lib.elmo_int8_matmul.restype = _I
+_lib.elmo_int8_matmul.argtypes = [_P, _L, _P, _P, _L, _P, _P, _L, _L, _L, _P, _L, _I, _P]
+_lib.elmo_sample_bytes.restype = _Z
+_lib.elmo_sample_bytes.argtypes = [_L, _L]
+_lib.elmo_sample.restype = _I
+_lib.elmo_sample.argtypes = [_P, _L, _I, _L, _L, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]
+_lib.elmo_distill_bytes.restype = _Z
+_lib.elmo_distill_bytes.argtypes = [_L, _L]
+_lib.elmo_distill.restype = _I
+_lib.elmo_distill.argtypes = [_P, _L, _I, _L, _L, _P, _P, _I, _L, _F, _P, _P, _P, _L, _P, _Z, _P]
 
 EXPORTS = ("elmo_last_error", "elmo_logit_buffer_bytes", "elmo_head_sizes", "elmo_head_create",
            "elmo_head_step", "elmo_head_topk", "elmo_head_destroy", "elmo_quantize", "elmo_philox4x32_10",
            "elmo_head_profile", "elmo_head_profile_read", "elmo_precision_hits", "elmo_quantize_em",
-           "elmo_dropout_keep16", "elmo_kahan_adamw", "elmo_topk_static")
+           "elmo_dropout_keep16", "elmo_kahan_adamw", "elmo_topk_static", "elmo_rms_norm",
+           "elmo_rms_norm_backward_bytes", "elmo_rms_norm_backward", "elmo_int8_matmul", "elmo_sample_bytes", "elmo_sample",
+           "elmo_distill_bytes", "elmo_distill")
 
 
 def _check(rc: int) -> None:
@@ -197,6 +217,162 @@ def elmo_philox4x32_10(ctr, key):
     o = (C.c_uint32 * 4)()
     _lib.elmo_philox4x32_10(c, k, o)
     return list(o)
+
+
+# ------------------------------------------------------------------ the output end of a language model
+# These take shapes, strides and types from the tensors and refuse (ElmoError -1 / -2) what does not fit together.  BF16 values are
+# torch.bfloat16 or their bit patterns as torch.int16, E4M3 codes torch.float8_e4m3fn or torch.uint8.  The work runs on the tensors' own
+# device, on `stream` or that device's current one.  A workspace that is not given is allocated for the call on that stream.
+_REAL = {torch.bfloat16: ELMO_BF16, torch.int16: ELMO_BF16, torch.float32: ELMO_FP32}
+_ROWS = {**_REAL, torch.float8_e4m3fn: ELMO_FP8_E4M3, torch.uint8: ELMO_FP8_E4M3, torch.int8: ELMO_INT8}
+_ONLY_FP32, _ONLY_INT32, _ONLY_INT8 = {torch.float32: ELMO_FP32}, {torch.int32: 0}, {torch.int8: ELMO_INT8}
+
+
+def _matrix(name, t, types, rows=None, cols=None):
+    """(address, row stride, type code) of a 2-D tensor whose rows are dense; (None, 0, 0) for None."""
+    if t is None:
+        return None, 0, 0
+    code = types.get(t.dtype)
+    if code is None:
+        raise ElmoError(-2, f"{name}: unsupported dtype {t.dtype}")
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ElmoError(-1, f"{name}: shape {tuple(t.shape)}, expected ({'rows' if rows is None else rows}, {'columns' if cols is None else cols})")
+    stride, step = t.stride()
+    if step != 1 and t.shape[1] > 1:
+        raise ElmoError(-1, f"{name}: the elements of a row must lie next to each other (stride {step})")
+    return t.data_ptr(), stride, code
+
+
+def _vector(name, t, types, n):
+    """(address, type code) of a dense 1-D tensor of n elements; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    code = types.get(t.dtype)
+    if code is None:
+        raise ElmoError(-2, f"{name}: unsupported dtype {t.dtype}")
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ElmoError(-1, f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, expected {n} dense elements")
+    return t.data_ptr(), code
+
+
+def _needed(**tensors):
+    for name, t in tensors.items():
+        if t is None:
+            raise ElmoError(-1, f"{name} is missing")
+
+
+def _call(fn, args, tensors, stream, workspace=None, bytes_needed=None):
+    """fn(*args[, workspace, its size], stream) on the device that holds all `tensors`."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ElmoError(-1, f"tensors on {t.device} and {device}")
+    if device.type != "cuda":
+        raise ElmoError(-1, f"the tensors must be on the GPU (got {device})")
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(fn, args, tensors, stream, workspace, bytes_needed)
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    if bytes_needed is None:
+        return _check(fn(*args, stream.cuda_stream))
+    if workspace is None and bytes_needed:
+        with torch.cuda.stream(stream):     # the caching allocator then reuses it in this stream's order
+            workspace = torch.empty(bytes_needed, dtype=torch.uint8, device=device)
+    elif workspace is not None:
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ElmoError(-1, f"workspace: a dense tensor on {device} is needed")
+    return _check(fn(*args, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), stream.cuda_stream))
+
+
+def elmo_rms_norm(x, y, weight=None, eps=1e-6, *, residual=None, sum_out=None, scale_out=None, stream=None) -> None:
+    """y <- weight * h / sqrt(mean(h^2) + eps), h = x + residual; sum_out <- h; 8-bit y (int8, E4M3): scale_out <- the rows' scales."""
+    _needed(x=x, y=y)
+    xp, xs, dtype = _matrix("x", x, _REAL)
+    rows, d = x.shape
+    real = {k: v for k, v in _REAL.items() if v == dtype}
+    rp, rs, _ = _matrix("residual", residual, real, rows, d)
+    sp, ss, _ = _matrix("sum_out", sum_out, real, rows, d)
+    yp, ys, yt = _matrix("y", y, _ROWS, rows, d)
+    wp, wt = _vector("weight", weight, _REAL, d)
+    cp, _ = _vector("scale_out", scale_out, _ONLY_FP32, rows)
+    _call(_lib.elmo_rms_norm, (xp, xs, dtype, rows, d, rp, rs, wp, wt, eps, sp, ss, yp, ys, yt, cp),
+          (x, y, weight, residual, sum_out, scale_out), stream)
+
+
+def elmo_rms_norm_backward_bytes(rows, d) -> int:
+    return int(_lib.elmo_rms_norm_backward_bytes(rows, d))
+
+
+def elmo_rms_norm_backward(dy, h, dh, weight=None, eps=1e-6, *, dsum=None, dweight=None, workspace=None, stream=None) -> None:
+    """dh <- gradient of h (plus dsum), dweight <- gradient of the weight."""
+    _needed(dy=dy, h=h, dh=dh)
+    yp, ys, dtype = _matrix("dy", dy, _REAL)
+    rows, d = dy.shape
+    real = {k: v for k, v in _REAL.items() if v == dtype}
+    hp, hs, _ = _matrix("h", h, real, rows, d)
+    op, os_, _ = _matrix("dh", dh, real, rows, d)
+    sp, ss, _ = _matrix("dsum", dsum, real, rows, d)
+    wp, wt = _vector("weight", weight, _REAL, d)
+    gp, _ = _vector("dweight", dweight, _ONLY_FP32, d)
+    _call(_lib.elmo_rms_norm_backward, (yp, ys, hp, hs, dtype, rows, d, wp, wt, eps, sp, ss, op, os_, gp),
+          (dy, h, dh, weight, dsum, dweight), stream, workspace, 0 if dweight is None else elmo_rms_norm_backward_bytes(rows, d))
+
+
+def elmo_int8_matmul(a, a_scale, b, b_scale, out, bias=None, *, stream=None) -> None:
+    """out[m, n] <- (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]."""
+    _needed(a=a, a_scale=a_scale, b=b, b_scale=b_scale, out=out)
+    ap, as_, _ = _matrix("a", a, _ONLY_INT8)
+    M, K = a.shape
+    bp, bs, _ = _matrix("b", b, _ONLY_INT8, None, K)
+    N = b.shape[0]
+    op, os_, ot = _matrix("out", out, _REAL, M, N)
+    pa, _ = _vector("a_scale", a_scale, _ONLY_FP32, M)
+    pb, _ = _vector("b_scale", b_scale, _ONLY_FP32, N)
+    pc, _ = _vector("bias", bias, _ONLY_FP32, N)
+    _call(_lib.elmo_int8_matmul, (ap, as_, pa, bp, bs, pb, pc, M, N, K, op, os_, ot), (a, a_scale, b, b_scale, out, bias), stream)
+
+
+def elmo_sample_bytes(rows, V) -> int:
+    return int(_lib.elmo_sample_bytes(rows, V))
+
+
+def elmo_sample(logits, u, idx_out, *, temperature=None, top_k=None, top_p=None, min_p=None, prob_out=None, workspace=None, stream=None) -> None:
+    """idx_out <- one token a row by temperature, top-k, top-p and min-p from the random numbers u; prob_out <- its probability among the kept."""
+    _needed(logits=logits, u=u, idx_out=idx_out)
+    zp, zs, dtype = _matrix("logits", logits, _REAL)
+    rows, V = logits.shape
+    up, _ = _vector("u", u, _ONLY_FP32, rows)
+    tp, _ = _vector("temperature", temperature, _ONLY_FP32, rows)
+    kp, _ = _vector("top_k", top_k, _ONLY_INT32, rows)
+    pp, _ = _vector("top_p", top_p, _ONLY_FP32, rows)
+    mp, _ = _vector("min_p", min_p, _ONLY_FP32, rows)
+    ip, _ = _vector("idx_out", idx_out, _ONLY_INT32, rows)
+    qp, _ = _vector("prob_out", prob_out, _ONLY_FP32, rows)
+    _call(_lib.elmo_sample, (zp, zs, dtype, rows, V, up, tp, kp, pp, mp, ip, qp), (logits, u, idx_out, temperature, top_k, top_p, min_p, prob_out),
+          stream, workspace, elmo_sample_bytes(rows, V))
+
+
+def elmo_distill_bytes(rows, V) -> int:
+    return int(_lib.elmo_distill_bytes(rows, V))
+
+
+def elmo_distill(logits, teacher_idx, teacher_logits, loss_out, grad_out=None, *, temperature=1.0, row_weight=None, workspace=None,
+                 stream=None) -> None:
+    """loss_out <- row_weight T^2 KL(teacher's top tokens || student) for each row, grad_out <- its gradient by the logits."""
+    _needed(logits=logits, teacher_idx=teacher_idx, teacher_logits=teacher_logits, loss_out=loss_out)
+    zp, zs, dtype = _matrix("logits", logits, _REAL)
+    rows, V = logits.shape
+    tp, ts, _ = _matrix("teacher_idx", teacher_idx, _ONLY_INT32, rows)
+    K = teacher_idx.shape[1]
+    lp, ls, lt = _matrix("teacher_logits", teacher_logits, _REAL, rows, K)
+    if rows > 1 and (ts != K or ls != K):
+        raise ElmoError(-1, "teacher_idx and teacher_logits must be dense")
+    gp, gs, _ = _matrix("grad_out", grad_out, {k: v for k, v in _REAL.items() if v == dtype}, rows, V)
+    op, _ = _vector("loss_out", loss_out, _ONLY_FP32, rows)
+    vp, _ = _vector("row_weight", row_weight, _ONLY_FP32, rows)
+    _call(_lib.elmo_distill, (zp, zs, dtype, rows, V, tp, lp, lt, K, temperature, vp, op, gp, gs),
+          (logits, teacher_idx, teacher_logits, loss_out, grad_out, row_weight), stream, workspace, elmo_distill_bytes(rows, V))
 
 
 # ------------------------------------------------------------------ convenience owner of the buffers

@@ -3,11 +3,14 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libelmo_head.so")
-SOURCES = [os.path.join(HERE, "csrc", "elmo_head.hip")]
-HEADERS = [os.path.join(HERE, "csrc", h) for h in ("numerics.h", "tiles.h", "kernels.h", "topk_levels.h", "plan.h", "topk.h")] + [
+SOURCES = [os.path.join(HERE, "csrc", s) for s in ("elmo_head.hip", "elmo_lm.hip")]
+HEADERS = [os.path.join(HERE, "csrc", h) for h in ("errors.h", "numerics.h", "tiles.h", "kernels.h", "topk_levels.h", "plan.h", "topk.h",
+                                                   "rows.h", "norm.h", "int8.h", "sample.h", "distill.h")] + [
     os.path.join(os.path.dirname(HERE), "include", "elmo_head.h")]
 
 HIPCC_FLAGS = [
@@ -20,15 +23,23 @@ HIPCC_FLAGS = [
 ]
 
 
-def build(verbose: bool = False) -> str:
-    """Compile unconditionally; returns the path of the shared library."""
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, "-o", LIB_PATH, *SOURCES]
+def _hipcc(args: list[str], verbose: bool) -> None:
+    cmd = [os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile unconditionally, the sources side by side; returns the path of the shared library."""
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            list(pool.map(lambda so: _hipcc([*flags, "-c", so[0], "-o", so[1]], verbose), zip(SOURCES, objects)))
+        _hipcc(["--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB_PATH], verbose)
     return LIB_PATH
 
 

@@ -5,13 +5,12 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <mutex>
 #include <new>
 #include <vector>
 
+#include "errors.h"
 #include "kernels.h"
 #include "plan.h"
 #include "topk.h"
@@ -24,21 +23,9 @@ using elmo::align256;
 using elmo::round_up;
 using elmo::lay_out;
 
-thread_local char g_err[512] = "";
-
-int fail(int code, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return code;
-}
-
-#define ELMO_HIP(call)                                                                       \
-  do {                                                                                       \
-    hipError_t e_ = (call);                                                                  \
-    if (e_ != hipSuccess) return fail(-3, "%s failed: %s", #call, hipGetErrorString(e_));    \
-  } while (0)
+using elmo::g_err;
+using elmo::fail;
+using elmo::check_launch;
 
 int make_plan(int64_t L, int d, int fmt, int64_t chunk, int maxB, int64_t max_nnz, uint32_t flags, int64_t kahan_rows, Plan& p) {
   if (L < 1) return fail(-1, "L must be >= 1 (got %lld)", (long long)L);
@@ -64,12 +51,6 @@ int make_plan(int64_t L, int d, int fmt, int64_t chunk, int maxB, int64_t max_nn
   p.weight_decay = 0.0f;
   p.drop_thresh = 0;
   lay_out(p);
-  return 0;
-}
-
-int check_launch(const char* what) {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(-3, "launch of %s failed: %s", what, hipGetErrorString(e));
   return 0;
 }
 

@@ -1,0 +1,244 @@
+// C ABI of the operators at the output end of a language model (see include/elmo_head.h): norm, 8-bit integer product, sampling,
+// distillation.
+#include "../../include/elmo_head.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "distill.h"
+#include "errors.h"
+#include "int8.h"
+#include "norm.h"
+#include "sample.h"
+
+namespace {
+
+using elmo::check_launch;
+using elmo::fail;
+
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;      // rows of a launch
+constexpr int kNormMostD = 65536;                          // what a workgroup's registers hold
+
+int check_rows(const char* what, int64_t rows, int64_t n, int64_t most) {
+  if (rows < 0 || rows > kMostRows) return fail(-1, "%s: rows = %lld outside [0, 2^31)", what, (long long)rows);
+  if (n < 1 || n > most) return fail(-1, "%s: row length %lld outside [1, %lld]", what, (long long)n, (long long)most);
+  return 0;
+}
+int check_stride(const char* what, int64_t stride, int64_t n, int64_t rows) {
+  if (rows > 1 && stride < n) return fail(-1, "%s = %lld is less than a row's %lld elements", what, (long long)stride, (long long)n);
+  if (stride < 0 || stride > ((int64_t)1 << 40)) return fail(-1, "%s = %lld outside [0, 2^40]", what, (long long)stride);
+  return 0;
+}
+bool is_real(int dtype) { return dtype == ELMO_BF16 || dtype == ELMO_FP32; }
+int check_aligned(const char* what, const void* p, int dtype) {
+  const uintptr_t size = dtype == ELMO_FP32 ? 4 : dtype == ELMO_BF16 ? 2 : 1;
+  if ((uintptr_t)p & (size - 1)) return fail(-1, "%s must be aligned to its elements", what);
+  return 0;
+}
+#define ELMO_TRY(call) do { if (int rc_ = (call)) return rc_; } while (0)
+
+// ---- norm: waves of a row and octets of a lane.  One wave keeps a row of up to 4096 elements without a barrier; where the rows are
+// too few to fill the chip that way, four waves share one and each has a quarter of the work.
+struct RowShape { int wpr, steps; };
+RowShape norm_shape(int64_t rows, int d) {
+  const bool many = rows >= 4096;
+  if (d <= (many ? 4096 : 512)) return {1, (d + 511) / 512};
+  if (d <= 8192) return {4, (d + 2047) / 2048};
+  return {16, (d + 8191) / 8192};
+}
+int pow2_at_least(int n) { int p = 1; while (p < n) p *= 2; return p; }
+
+template <class T, int OUT, int WPR, int S> void launch_norm(const elmo::NormArgs& a, hipStream_t st) {
+  constexpr int threads = elmo::norm_threads(WPR), rpg = threads / (64 * WPR);
+  elmo::k_rms_norm<T, OUT, WPR, S><<<(unsigned)((a.rows + rpg - 1) / rpg), threads, 0, st>>>(a);
+}
+template <class T, int OUT> void launch_norm_shape(const elmo::NormArgs& a, hipStream_t st) {
+  const RowShape r = norm_shape(a.rows, a.d);
+  const int s = pow2_at_least(r.steps);
+#define ELMO_NORM(W, S) if (r.wpr == W && s == S) return launch_norm<T, OUT, W, S>(a, st)
+  ELMO_NORM(1, 1); ELMO_NORM(1, 2); ELMO_NORM(1, 4); ELMO_NORM(1, 8);
+  ELMO_NORM(4, 1); ELMO_NORM(4, 2); ELMO_NORM(4, 4);
+  ELMO_NORM(16, 2); ELMO_NORM(16, 4); ELMO_NORM(16, 8);
+#undef ELMO_NORM
+}
+template <class T> void launch_norm_out(const elmo::NormArgs& a, int out, hipStream_t st) {
+  if (out == ELMO_BF16) launch_norm_shape<T, elmo::OUT_BF16>(a, st);
+  else if (out == ELMO_FP32) launch_norm_shape<T, elmo::OUT_FP32>(a, st);
+  else if (out == ELMO_FP8_E4M3) launch_norm_shape<T, elmo::OUT_E4M3>(a, st);
+  else launch_norm_shape<T, elmo::OUT_INT8>(a, st);
+}
+
+// Backward: a team of waves keeps its columns' share of the weight gradient over all rows it takes.
+constexpr int kNormTeams = 1024;
+RowShape back_shape(int d) {
+  if (d <= 1024) return {1, (d + 511) / 512};
+  if (d <= 8192) return {4, (d + 2047) / 2048};
+  return {16, (d + 8191) / 8192};
+}
+int back_teams(int64_t rows) { return (int)std::min<int64_t>(rows, kNormTeams); }
+template <class T, int WPR, int S> void launch_back(const elmo::NormBackArgs& a, hipStream_t st) {
+  constexpr int threads = elmo::norm_threads(WPR), rpg = threads / (64 * WPR);
+  elmo::k_rms_norm_back<T, WPR, S><<<(a.teams + rpg - 1) / rpg, threads, 0, st>>>(a);
+}
+template <class T> void launch_back_shape(const elmo::NormBackArgs& a, hipStream_t st) {
+  const RowShape r = back_shape(a.d);
+  const int s = pow2_at_least(r.steps);
+#define ELMO_BACK(W, S) if (r.wpr == W && s == S) return launch_back<T, W, S>(a, st)
+  ELMO_BACK(1, 1); ELMO_BACK(1, 2);
+  ELMO_BACK(4, 1); ELMO_BACK(4, 2); ELMO_BACK(4, 4);
+  ELMO_BACK(16, 2); ELMO_BACK(16, 4); ELMO_BACK(16, 8);
+#undef ELMO_BACK
+}
+
+}  // namespace
+
+extern "C" int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int64_t d, const void* residual, int64_t residual_stride,
+                             const void* weight, int weight_dtype, float eps, void* sum_out, int64_t sum_stride, void* y, int64_t y_stride,
+                             int y_dtype, float* scale_out, void* hip_stream) {
+  if (!is_real(dtype)) return fail(-2, "dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", dtype);
+  if (weight && !is_real(weight_dtype)) return fail(-2, "weight_dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", weight_dtype);
+  if (!is_real(y_dtype) && y_dtype != ELMO_FP8_E4M3 && y_dtype != ELMO_INT8) return fail(-2, "unsupported y_dtype %d", y_dtype);
+  ELMO_TRY(check_rows("elmo_rms_norm", rows, d, kNormMostD));
+  if (!(eps >= 0.0f) || eps > 1e30f) return fail(-1, "eps must be >= 0 and finite (got %g)", (double)eps);
+  if (rows == 0) return 0;
+  if (!x || !y) return fail(-1, "x and y must not be NULL");
+  if (sum_out && !residual) return fail(-1, "sum_out needs a residual");
+  if (!is_real(y_dtype) && !scale_out) return fail(-1, "8-bit rows need scale_out");
+  if (is_real(y_dtype) && scale_out) return fail(-1, "scale_out goes with 8-bit rows only");
+  ELMO_TRY(check_stride("x_stride", x_stride, d, rows));
+  ELMO_TRY(check_stride("y_stride", y_stride, d, rows));
+  if (residual) ELMO_TRY(check_stride("residual_stride", residual_stride, d, rows));
+  if (sum_out) ELMO_TRY(check_stride("sum_stride", sum_stride, d, rows));
+  ELMO_TRY(check_aligned("x", x, dtype));
+  ELMO_TRY(check_aligned("residual", residual, dtype));
+  ELMO_TRY(check_aligned("sum_out", sum_out, dtype));
+  ELMO_TRY(check_aligned("weight", weight, weight_dtype));
+  ELMO_TRY(check_aligned("y", y, y_dtype));
+  ELMO_TRY(check_aligned("scale_out", scale_out, ELMO_FP32));
+  const elmo::NormArgs a{x, residual, weight, sum_out, y, scale_out, rows, x_stride, residual_stride, sum_stride, y_stride, (int)d, eps,
+                         weight_dtype == ELMO_FP32};
+  if (dtype == ELMO_BF16) launch_norm_out<uint16_t>(a, y_dtype, (hipStream_t)hip_stream);
+  else launch_norm_out<float>(a, y_dtype, (hipStream_t)hip_stream);
+  return check_launch("k_rms_norm");
+}
+
+extern "C" size_t elmo_rms_norm_backward_bytes(int64_t rows, int64_t d) {
+  return rows < 1 || d < 1 || d > kNormMostD ? 0 : (size_t)back_teams(rows) * (size_t)d * sizeof(float);
+}
+
+extern "C" int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int64_t h_stride, int dtype, int64_t rows, int64_t d,
+                                      const void* weight, int weight_dtype, float eps, const void* dsum, int64_t dsum_stride, void* dh,
+                                      int64_t dh_stride, float* dweight, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!is_real(dtype)) return fail(-2, "dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", dtype);
+  if (weight && !is_real(weight_dtype)) return fail(-2, "weight_dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", weight_dtype);
+  ELMO_TRY(check_rows("elmo_rms_norm_backward", rows, d, kNormMostD));
+  if (!(eps >= 0.0f) || eps > 1e30f) return fail(-1, "eps must be >= 0 and finite (got %g)", (double)eps);
+  ELMO_TRY(check_aligned("dweight", dweight, ELMO_FP32));
+  hipStream_t st = (hipStream_t)hip_stream;
+  const int teams = back_teams(rows);
+  if (rows > 0) {
+    if (!dy || !h || !dh) return fail(-1, "dy, h and dh must not be NULL");
+    ELMO_TRY(check_stride("dy_stride", dy_stride, d, rows));
+    ELMO_TRY(check_stride("h_stride", h_stride, d, rows));
+    ELMO_TRY(check_stride("dh_stride", dh_stride, d, rows));
+    if (dsum) ELMO_TRY(check_stride("dsum_stride", dsum_stride, d, rows));
+    ELMO_TRY(check_aligned("dy", dy, dtype));
+    ELMO_TRY(check_aligned("h", h, dtype));
+    ELMO_TRY(check_aligned("dh", dh, dtype));
+    ELMO_TRY(check_aligned("dsum", dsum, dtype));
+    ELMO_TRY(check_aligned("weight", weight, weight_dtype));
+    if (dweight && (!workspace || workspace_bytes < elmo_rms_norm_backward_bytes(rows, d)))
+      return fail(-1, "workspace missing or smaller than %zu bytes", elmo_rms_norm_backward_bytes(rows, d));
+    if (dweight) ELMO_TRY(check_aligned("workspace", workspace, ELMO_FP32));
+    const elmo::NormBackArgs a{dy, h, weight, dsum, dh, dweight ? (float*)workspace : nullptr, rows, dy_stride, h_stride, dsum_stride, dh_stride,
+                               (int)d, teams, eps, weight_dtype == ELMO_FP32};
+    if (dtype == ELMO_BF16) launch_back_shape<uint16_t>(a, st);
+    else launch_back_shape<float>(a, st);
+    ELMO_TRY(check_launch("k_rms_norm_back"));
+  }
+  if (!dweight) return 0;
+  elmo::k_norm_dweight<<<(unsigned)((d + 63) / 64), 64 * elmo::kDweightWaves, 0, st>>>((const float*)workspace, teams, (int)d, dweight);
+  return check_launch("k_norm_dweight");
+}
+
+extern "C" int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, const int8_t* b, int64_t b_stride, const float* b_scale,
+                                const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t out_stride, int out_dtype,
+                                void* hip_stream) {
+  constexpr int64_t most = (int64_t)1 << 30, most_k = 131071;      // 131071 products of 128 x 128 stay below 2^31
+  if (!is_real(out_dtype)) return fail(-2, "out_dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", out_dtype);
+  if (M < 0 || M > most || N < 0 || N > most) return fail(-1, "M = %lld and N = %lld must be in [0, 2^30]", (long long)M, (long long)N);
+  if (K < 0 || K > most_k) return fail(-1, "K = %lld outside [0, %lld]: longer sums do not fit 32 bits", (long long)K, (long long)most_k);
+  if (M == 0 || N == 0) return 0;
+  if ((K > 0 && (!a || !b)) || !a_scale || !b_scale || !out) return fail(-1, "a, b, a_scale, b_scale and out must not be NULL");
+  ELMO_TRY(check_stride("a_stride", a_stride, K, M));
+  ELMO_TRY(check_stride("b_stride", b_stride, K, N));
+  ELMO_TRY(check_stride("out_stride", out_stride, N, M));
+  ELMO_TRY(check_aligned("a_scale", a_scale, ELMO_FP32));
+  ELMO_TRY(check_aligned("b_scale", b_scale, ELMO_FP32));
+  ELMO_TRY(check_aligned("bias", bias, ELMO_FP32));
+  ELMO_TRY(check_aligned("out", out, out_dtype));
+  const elmo::Int8Args p{(const char*)a, (const char*)b, a_scale, b_scale, bias, out, a_stride, b_stride, out_stride, (int)M, (int)N, (int)K};
+  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
+  if (tiles > kMostRows) return fail(-1, "M x N = %lld x %lld is more than one launch takes", (long long)M, (long long)N);
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (out_dtype == ELMO_BF16) elmo::k_int8_plain<uint16_t><<<(unsigned)tiles, elmo::kThreads, 0, st>>>(p);
+  else elmo::k_int8_plain<float><<<(unsigned)tiles, elmo::kThreads, 0, st>>>(p);
+  return check_launch("k_int8_plain");
+}
+
+namespace {
+constexpr int64_t kMostV = ((int64_t)1 << 31) - 1;
+}
+
+extern "C" size_t elmo_sample_bytes(int64_t rows, int64_t V) { return 0; }
+
+extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const float* u, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p, int32_t* idx_out, float* prob_out, void* workspace,
+                           size_t workspace_bytes, void* hip_stream) {
+  if (!is_real(dtype)) return fail(-2, "dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", dtype);
+  ELMO_TRY(check_rows("elmo_sample", rows, V, kMostV));
+  if (rows == 0) return 0;
+  if (!logits || !u || !idx_out) return fail(-1, "logits, u and idx_out must not be NULL");
+  ELMO_TRY(check_stride("logits_stride", logits_stride, V, rows));
+  ELMO_TRY(check_aligned("logits", logits, dtype));
+  for (const void* p : {(const void*)u, (const void*)temperature, (const void*)top_k, (const void*)top_p, (const void*)min_p, (const void*)idx_out,
+                        (const void*)prob_out})
+    ELMO_TRY(check_aligned("u, temperature, top_k, top_p, min_p, idx_out and prob_out", p, ELMO_FP32));
+  int bits = 0;
+  while (((int64_t)1 << bits) < V) ++bits;
+  const elmo::SampleArgs a{logits, logits_stride, V, u, temperature, top_p, min_p, top_k, idx_out, prob_out, std::min(50, 62 - bits)};
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (dtype == ELMO_BF16) elmo::k_sample_plain<uint16_t><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
+  else elmo::k_sample_plain<float><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
+  return check_launch("k_sample_plain");
+}
+
+extern "C" size_t elmo_distill_bytes(int64_t rows, int64_t V) { return 0; }
+
+extern "C" int elmo_distill(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const int32_t* teacher_idx,
+                            const void* teacher_logits, int teacher_dtype, int64_t K, float temperature, const float* row_weight, float* loss_out,
+                            void* grad_out, int64_t grad_stride, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!is_real(dtype)) return fail(-2, "dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", dtype);
+  if (!is_real(teacher_dtype)) return fail(-2, "teacher_dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", teacher_dtype);
+  ELMO_TRY(check_rows("elmo_distill", rows, V, kMostV));
+  if (K < 1 || K > elmo::kDistillMaxK) return fail(-1, "K = %lld outside [1, %d]", (long long)K, elmo::kDistillMaxK);
+  if (!(temperature > 0.0f) || !(temperature <= 1e6f) || temperature < 1e-6f) return fail(-1, "temperature must be in [1e-6, 1e6] (got %g)", (double)temperature);
+  if (rows == 0) return 0;
+  if (!logits || !teacher_idx || !teacher_logits || !loss_out) return fail(-1, "logits, teacher_idx, teacher_logits and loss_out must not be NULL");
+  ELMO_TRY(check_stride("logits_stride", logits_stride, V, rows));
+  if (grad_out) ELMO_TRY(check_stride("grad_stride", grad_stride, V, rows));
+  ELMO_TRY(check_aligned("logits", logits, dtype));
+  ELMO_TRY(check_aligned("grad_out", grad_out, dtype));
+  ELMO_TRY(check_aligned("teacher_logits", teacher_logits, teacher_dtype));
+  for (const void* p : {(const void*)teacher_idx, (const void*)row_weight, (const void*)loss_out})
+    ELMO_TRY(check_aligned("teacher_idx, row_weight and loss_out", p, ELMO_FP32));
+  const elmo::DistillArgs a{logits, teacher_idx, teacher_logits, row_weight, loss_out, grad_out, logits_stride, grad_stride, V, (int)K, temperature,
+                            (float)(1.4426950408889634 / (double)temperature), teacher_dtype == ELMO_FP32};
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (dtype == ELMO_BF16) elmo::k_distill_plain<uint16_t><<<(unsigned)rows, elmo::kDistillThreads, 0, st>>>(a);
+  else elmo::k_distill_plain<float><<<(unsigned)rows, elmo::kDistillThreads, 0, st>>>(a);
+  return check_launch("k_distill_plain");
+}
