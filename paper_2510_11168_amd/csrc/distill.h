@@ -10,8 +10,7 @@
 namespace elmo {
 
 constexpr int kDistillMaxK = 1024;
-constexpr int kDistillThreads = 1024;
-constexpr double kLn2 = 0.6931471805599453;
+constexpr int kDistillThreads = 512;
 
 struct DistillArgs {
   const void* z;
@@ -21,107 +20,185 @@ struct DistillArgs {
   float* loss;
   void* grad;                        // NULL: none
   int64_t zs, gs;                    // row strides in elements
-  int64_t V;
+  int64_t rows, V;
   int K;
   float T, c;                        // c = log2(e) / T
   bool t32;                          // FP32 teacher logits
+  int parts;                         // workgroups of a row
+  void* ws;                          // of split rows: [rows, parts] MaxSum, [rows, kDistillMaxK] logits of the teacher's tokens
 };
 
-// (maximum, sum of exp2((z - m) c)) of two parts of a row.  A part without a finite logit has m = -infinity and no sum.
+// (maximum, sum of exp2(z c - shift(m, c))) of a part of a row.  A part without a finite logit has m = -infinity and no sum.  Parts are
+// joined by the difference of their rounded shifts, those that their sums were taken with.
 struct MaxSum { float m, s; };
 __device__ inline float shift(float m, float c) { return m == -__builtin_inff() ? 0.0f : m * c; }
-__device__ inline MaxSum join(MaxSum a, MaxSum b, float c) {
-  const float m = fmaxf(a.m, b.m), mc = shift(m, c);
-  return {m, a.s * __builtin_amdgcn_exp2f(__builtin_fmaf(a.m, c, -mc)) + b.s * __builtin_amdgcn_exp2f(__builtin_fmaf(b.m, c, -mc))};
+__device__ inline float rescale(float m, float c, float mc) { return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m * c - mc); }
+
+// The exponentials of an octet against shift mc, summed.
+template <class T> __device__ inline float octet_sum(const Octet<T>& o, float c, float mc) {
+  float e[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(o[i], c, -mc));
+  return ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+}
+template <class T> __device__ inline float octet_max(const Octet<T>& o) {
+  return fmaxf(fmaxf(fmaxf(o[0], o[1]), fmaxf(o[2], o[3])), fmaxf(fmaxf(o[4], o[5]), fmaxf(o[6], o[7])));
+}
+// Octets [lo, hi) of part `part` of `parts`, in whole rounds of a workgroup.
+struct Range { int64_t lo, hi; };
+__device__ inline Range part_of(int64_t octets, int part, int parts) {
+  const int64_t rounds = (octets + kDistillThreads - 1) / kDistillThreads, per = (rounds + parts - 1) / parts;
+  const int64_t lo = min(octets, per * part * kDistillThreads);
+  return {lo, min(octets, lo + per * kDistillThreads)};
 }
 
-template <class T>
-__global__ __launch_bounds__(kDistillThreads) void k_distill_plain(DistillArgs a) {
-  constexpr int NW = kDistillThreads / 64;
-  __shared__ float s_m[NW], s_s[NW];
-  __shared__ double s_d[NW];
-  __shared__ float s_q[kDistillMaxK], s_z[kDistillMaxK];
+// WHOLE: a row a workgroup.  It is read twice -- 256 rows of a large vocabulary that are worked on at a time fit the memory-side cache, from
+// which the second reading comes -- and the gradient goes past the caches.  4096 x 131072 BF16: 557 us, 3.9 TB/s of what has to move (a copy:
+// 4.8); rows held in registers, with the next one's loads under way as the gradient is written: 559 to 600.
+// SUMS, GRADIENT: few rows, in `parts` workgroups each: the parts' maxima and sums with the teacher's tokens' logits, then the gradient with them.  (The
+// second launch takes no logit that another part may already have overwritten.)  One row of 131072: see the launch.
+enum : int { DISTILL_WHOLE = 0, DISTILL_SUMS = 1, DISTILL_GRADIENT = 2 };
+template <class T, int MODE>
+__global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
+  constexpr int NT = kDistillThreads, NW = NT / 64, PER = kDistillMaxK / NT;
+  __shared__ float s_m[NW], s_s[NW], s_t[NW], s_q[kDistillMaxK], s_z[kDistillMaxK];
+  __shared__ double s_d[NW], s_l[NW], s_x[kDistillMaxK], s_e[kDistillMaxK];
   __shared__ int s_i[kDistillMaxK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = blockIdx.x;
+  const int64_t row = MODE == DISTILL_WHOLE ? blockIdx.x : blockIdx.x / a.parts;
+  const int part = MODE == DISTILL_WHOLE ? 0 : (int)(blockIdx.x % a.parts);
   const T* z = (const T*)a.z + row * a.zs;
   T* g = a.grad ? (T*)a.grad + row * a.gs : nullptr;
+  // whole octets; the up to seven elements behind them go to as many threads of the last part, one each
+  const int64_t octets = a.V >> 3, rest = octets * 8;
+  const Range r = MODE == DISTILL_WHOLE ? Range{0, octets} : part_of(octets, part, a.parts);
+  const int tail = part == a.parts - 1 ? (int)(a.V - rest) : 0;
+  MaxSum* partials = (MaxSum*)a.ws + row * a.parts;
+  float* token_z = (float*)((MaxSum*)a.ws + a.rows * a.parts) + row * kDistillMaxK;
   const float v = a.v ? a.v[row] : 1.0f;
-  // ---- teacher: q over the tokens that are there
-  int idx = -1;
-  float t = -__builtin_inff();
-  if (tid < a.K) {
-    idx = a.ti[row * a.K + tid];
-    if (idx < 0 || idx >= a.V) idx = -1;
-    else t = a.t32 ? ((const float*)a.tz)[row * a.K + tid] : bf16_decode(((const uint16_t*)a.tz)[row * a.K + tid]);
-    if (!(t == t)) t = __builtin_inff();   // NaN teacher: NaN loss and gradient, by inf - inf
+  // ---- the teacher's tokens and its largest logit
+  float m = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * NT + tid;
+    if (j < a.K) {
+      int at = a.ti[row * a.K + j];
+      float t = a.t32 ? ((const float*)a.tz)[row * a.K + j] : bf16_decode(((const uint16_t*)a.tz)[row * a.K + j]);
+      if (!(t == t)) t = __builtin_inff();               // a NaN teacher makes the row NaN, by inf - inf
+      if (at < 0 || at >= a.V) { at = -1; t = -__builtin_inff(); }
+      s_i[j] = at;
+      s_x[j] = (double)t;
+      if (MODE != DISTILL_GRADIENT) s_z[j] = at >= 0 && v != 0.0f ? load_one(z, at) : 0.0f;
+      else s_z[j] = v != 0.0f ? token_z[j] : 0.0f;
+      if (MODE == DISTILL_SUMS && part == 0 && v != 0.0f) token_z[j] = s_z[j];
+      m = fmaxf(m, t);
+    }
   }
-  float m = wave_max(t);
-  if (lane == 0) s_m[wave] = m;
+  m = wave_max(m);
+  if (lane == 0) s_t[wave] = m;
   __syncthreads();
-  m = s_m[0];
-  for (int i = 1; i < NW; ++i) m = fmaxf(m, s_m[i]);
-  if (m == -__builtin_inff() || v == 0.0f) {       // no teacher, or a row that does not count
-    if (g)
-      for (int64_t c = tid; c < a.V; c += kDistillThreads) store_one(g, c, 0.0f);
-    if (tid == 0) a.loss[row] = 0.0f;
+  m = slots_reduce<NW>(s_t, lane, [](float p, float q) { return fmaxf(p, q); });
+  if (m == -__builtin_inff() || v == 0.0f) {             // no teacher, or a row that does not count
+    if (MODE == DISTILL_SUMS) return;
+    if (g) {
+      const float zero[8] = {};
+      for (int64_t o = r.lo + tid; o < r.hi; o += NT) store_octet<true>(g + o * 8, 8, zero);
+      if (tid < tail) store_one(g, rest + tid, 0.0f);
+    }
+    if (tid == 0 && part == 0) a.loss[row] = 0.0f;
     return;
   }
-  const double x = ((double)t - (double)m) / (double)a.T;
-  double e = t == -__builtin_inff() ? 0.0 : exp(x);
-  double sum = wave_reduce(e, [](double p, double q) { return p + q; });
+  // ---- student: maximum and sum in one pass
+  const float last = tid < tail ? load_one(z, rest + tid) : -__builtin_inff();
+  MaxSum ms = {-__builtin_inff(), 0.0f};
+  if constexpr (MODE != DISTILL_GRADIENT) {
+    if (tid < tail) {
+      if (last == last) ms.m = last;                     // (a NaN is in the sum)
+      ms.s = __builtin_amdgcn_exp2f(__builtin_fmaf(last, a.c, -shift(ms.m, a.c)));
+    }
+#pragma unroll 4
+    for (int64_t o = r.lo + tid; o < r.hi; o += NT) {
+      const Octet<T> oc = load_octet(z + o * 8, 8);
+      const float top = octet_max(oc);
+      if (top > ms.m) ms = {top, ms.s * rescale(ms.m, a.c, shift(top, a.c))};
+      ms.s += octet_sum(oc, a.c, shift(ms.m, a.c));
+    }
+    const float top = wave_max(ms.m);
+    ms = {top, wave_sum(ms.s * rescale(ms.m, a.c, shift(top, a.c)))};
+    if (lane == 0) {
+      s_m[wave] = ms.m;
+      s_s[wave] = ms.s;
+    }
+    __syncthreads();
+    ms.m = slots_reduce<NW>(s_m, lane, [](float p, float q) { return fmaxf(p, q); });
+    ms.s = wave_reduce<NW>(s_s[lane & (NW - 1)] * rescale(s_m[lane & (NW - 1)], a.c, shift(ms.m, a.c)), [](float p, float q) { return p + q; });
+    if (MODE == DISTILL_SUMS) {
+      if (tid == 0) partials[part] = ms;
+      return;
+    }
+  } else {
+    const MaxSum mine = lane < a.parts ? partials[lane] : ms;    // (at most 64 parts)
+    ms.m = wave_max(mine.m);
+    ms.s = wave_sum(mine.s * rescale(mine.m, a.c, shift(ms.m, a.c)));
+  }
+  const float mc = shift(ms.m, a.c);
+  // ---- gradient: p everywhere
+  const float vT = v * a.T, inv = ms.s == 0.0f ? 0.0f : vT / ms.s;
+  const auto p_of = [&](float f) { return __builtin_amdgcn_exp2f(__builtin_fmaf(f, a.c, -mc)) * inv; };
+  if (g) {
+    if (tid < tail) store_one(g, rest + tid, p_of(last));
+#pragma unroll 4
+    for (int64_t o = r.lo + tid; o < r.hi; o += NT) {
+      const Octet<T> oc = load_octet(z + o * 8, 8);
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = p_of(oc[i]);
+      store_octet<true>(g + o * 8, 8, f);
+    }
+  }
+  // ---- loss: the teacher's q, and log p of its tokens
+  double sum = 0.0;
+#pragma unroll 1
+  for (int j = tid; j < a.K; j += NT) {
+    const double x = (s_x[j] - (double)m) / (double)a.T, e = s_x[j] == -__builtin_inf() ? 0.0 : exp_series(x);
+    s_x[j] = x;
+    s_e[j] = e;
+    sum += e;
+  }
+  sum = wave_reduce(sum, [](double p, double q) { return p + q; });
   if (lane == 0) s_d[wave] = sum;
   __syncthreads();
-  sum = 0.0;
-  for (int i = 0; i < NW; ++i) sum += s_d[i];
-  const double q = e / sum, logq = x - log(sum);
-  // ---- student: maximum and sum
-  float mine = -__builtin_inff(), part = 0.0f;
-  for (int64_t c = tid; c < a.V; c += kDistillThreads) mine = fmaxf(mine, load_one(z, c));
-  mine = wave_max(mine);
-  __syncthreads();
-  if (lane == 0) s_m[wave] = mine;
-  __syncthreads();
-  mine = s_m[0];
-  for (int i = 1; i < NW; ++i) mine = fmaxf(mine, s_m[i]);
-  const float mc = shift(mine, a.c);
-  for (int64_t c = tid; c < a.V; c += kDistillThreads) part += __builtin_amdgcn_exp2f(__builtin_fmaf(load_one(z, c), a.c, -mc));
-  part = wave_sum(part);
-  if (lane == 0) s_s[wave] = part;
-  const float zi = idx >= 0 ? load_one(z, idx) : 0.0f;
-  s_i[tid] = idx;
-  s_q[tid] = (float)q;
-  s_z[tid] = zi;
-  __syncthreads();
-  part = 0.0f;
-  for (int i = 0; i < NW; ++i) part += s_s[i];
-  // ---- loss
-  double term = 0.0;
-  if (idx >= 0 && q != 0.0) term = q * (logq - kLn2 * ((double)zi * (double)a.c - (double)mc) + log((double)part));
-  if (mine == -__builtin_inff()) term = idx >= 0 && q != 0.0 ? (double)__builtin_inff() : 0.0;
-  term = wave_reduce(term, [](double p, double q) { return p + q; });
-  __syncthreads();
-  if (lane == 0) s_d[wave] = term;
-  __syncthreads();
-  if (tid == 0) {
-    double l = 0.0;
-    for (int i = 0; i < NW; ++i) l += s_d[i];
-    a.loss[row] = (float)(l * (double)a.T * (double)a.T * (double)v);
+  sum = slots_reduce<NW>(s_d, lane, [](double p, double q) { return p + q; });
+  const double logsum = log_series(sum), lognorm = log_series((double)ms.s);
+  double loss = 0.0;
+#pragma unroll 1
+  for (int j = tid; j < a.K; j += NT) {
+    const double q = s_e[j] / sum;
+    if (s_i[j] >= 0 && !(q == 0.0))
+      loss += ms.m == -__builtin_inff() ? (double)__builtin_inff() : q * (s_x[j] - logsum - kLn2 * ((double)s_z[j] * (double)a.c - (double)mc) + lognorm);
+    s_q[j] = (float)q;
   }
+  loss = wave_reduce(loss, [](double p, double q) { return p + q; });
+  if (lane == 0) s_l[wave] = loss;
+  __syncthreads();                                       // also orders the octets' stores before the ones below
+  loss = slots_reduce<NW>(s_l, lane, [](double p, double q) { return p + q; });
+  if (tid == 0 && part == 0) a.loss[row] = (float)(loss * (double)a.T * (double)a.T * (double)v);
   if (!g) return;
-  // ---- gradient
-  const float scale = v * a.T, inv = part > 0.0f ? scale / part : part == 0.0f ? 0.0f : part;
-  for (int64_t c = tid; c < a.V; c += kDistillThreads) store_one(g, c, __builtin_amdgcn_exp2f(__builtin_fmaf(load_one(z, c), a.c, -mc)) * inv);
-  __syncthreads();
-  if (idx >= 0) {
+  // ---- the teacher's tokens once more (of equal ones the first, for all), each by the part that wrote it
+  const int64_t from = r.lo * 8, to = r.hi * 8 + tail;
+#pragma unroll 1
+  for (int k = tid; k < a.K; k += NT) {
+    const int at = s_i[k];
+    if (at < 0 || at < from || at >= to) continue;
     float all = 0.0f;
-    int first = tid;
+    int first = k;
+#pragma unroll 4
     for (int j = 0; j < a.K; ++j)
-      if (s_i[j] == idx) {
+      if (s_i[j] == at) {
         first = min(first, j);
         all += s_q[j];
       }
-    if (first == tid) store_one(g, idx, __builtin_amdgcn_exp2f(__builtin_fmaf(zi, a.c, -mc)) * inv - scale * all);
+    if (first == k) store_one(g, at, p_of(s_z[k]) - vT * all);
   }
 }
 

@@ -216,7 +216,33 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
   return check_launch("k_sample_plain");
 }
 
-extern "C" size_t elmo_distill_bytes(int64_t rows, int64_t V) { return 0; }
+namespace {
+// Workgroups of a row: one where the rows fill the chip or are short, else up to 64, each with at least one round of octets.
+int distill_parts(int64_t rows, int64_t V) {
+  const int64_t rounds = (V / 8 + elmo::kDistillThreads - 1) / elmo::kDistillThreads;
+  if (rows > 128 || rounds < 4) return 1;
+  const int64_t parts = std::min<int64_t>(std::min<int64_t>(rounds, 64), 512 / rows);
+  const int64_t per = (rounds + parts - 1) / parts;
+  return (int)((rounds + per - 1) / per);
+}
+template <class T> int launch_distill(const elmo::DistillArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)(a.rows * a.parts);
+  if (a.parts == 1) {
+    elmo::k_distill<T, elmo::DISTILL_WHOLE><<<grid, elmo::kDistillThreads, 0, st>>>(a);
+    return check_launch("k_distill");
+  }
+  elmo::k_distill<T, elmo::DISTILL_SUMS><<<grid, elmo::kDistillThreads, 0, st>>>(a);
+  ELMO_TRY(check_launch("k_distill (sums)"));
+  elmo::k_distill<T, elmo::DISTILL_GRADIENT><<<grid, elmo::kDistillThreads, 0, st>>>(a);
+  return check_launch("k_distill (gradient)");
+}
+}  // namespace
+
+extern "C" size_t elmo_distill_bytes(int64_t rows, int64_t V) {
+  if (rows < 1 || V < 1) return 0;
+  const int parts = distill_parts(rows, V);
+  return parts == 1 ? 0 : (size_t)rows * (parts * sizeof(elmo::MaxSum) + elmo::kDistillMaxK * sizeof(float));
+}
 
 extern "C" int elmo_distill(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const int32_t* teacher_idx,
                             const void* teacher_logits, int teacher_dtype, int64_t K, float temperature, const float* row_weight, float* loss_out,
@@ -235,10 +261,10 @@ extern "C" int elmo_distill(const void* logits, int64_t logits_stride, int dtype
   ELMO_TRY(check_aligned("teacher_logits", teacher_logits, teacher_dtype));
   for (const void* p : {(const void*)teacher_idx, (const void*)row_weight, (const void*)loss_out})
     ELMO_TRY(check_aligned("teacher_idx, row_weight and loss_out", p, ELMO_FP32));
-  const elmo::DistillArgs a{logits, teacher_idx, teacher_logits, row_weight, loss_out, grad_out, logits_stride, grad_stride, V, (int)K, temperature,
-                            (float)(1.4426950408889634 / (double)temperature), teacher_dtype == ELMO_FP32};
+  const size_t need = elmo_distill_bytes(rows, V);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return fail(-1, "workspace missing, smaller than %zu bytes or not 256-byte aligned", need);
+  const elmo::DistillArgs a{logits, teacher_idx, teacher_logits, row_weight, loss_out, grad_out, logits_stride, grad_stride, rows, V, (int)K, temperature,
+                            (float)(1.4426950408889634 / (double)temperature), teacher_dtype == ELMO_FP32, distill_parts(rows, V), workspace};
   hipStream_t st = (hipStream_t)hip_stream;
-  if (dtype == ELMO_BF16) elmo::k_distill_plain<uint16_t><<<(unsigned)rows, elmo::kDistillThreads, 0, st>>>(a);
-  else elmo::k_distill_plain<float><<<(unsigned)rows, elmo::kDistillThreads, 0, st>>>(a);
-  return check_launch("k_distill_plain");
+  return dtype == ELMO_BF16 ? launch_distill<uint16_t>(a, st) : launch_distill<float>(a, st);
 }

@@ -61,22 +61,30 @@ __device__ inline uint32_t pack_bf16(float a, float b) {
   p.h[1] = (__bf16)b;
   return p.u;
 }
-__device__ inline void store_octet(uint16_t* __restrict__ p, int64_t valid, const float (&f)[8]) {
+// NT: past the caches, for what nothing reads again soon.
+template <bool NT = false> __device__ inline void store_octet(uint16_t* __restrict__ p, int64_t valid, const float (&f)[8]) {
   u32x4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
   if (valid >= 8) {
-    *reinterpret_cast<u32x4_any2*>(p) = v;
+    if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any2*>(p));
+    else *reinterpret_cast<u32x4_any2*>(p) = v;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < valid) p[i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
   }
 }
-__device__ inline void store_octet(float* __restrict__ p, int64_t valid, const float (&f)[8]) {
+template <bool NT = false> __device__ inline void store_octet(float* __restrict__ p, int64_t valid, const float (&f)[8]) {
   if (valid >= 8) {
-    *reinterpret_cast<f32x4_any4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
-    *reinterpret_cast<f32x4_any4*>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+    const f32x4 a = {f[0], f[1], f[2], f[3]}, b = {f[4], f[5], f[6], f[7]};
+    if constexpr (NT) {
+      __builtin_nontemporal_store(a, reinterpret_cast<f32x4_any4*>(p));
+      __builtin_nontemporal_store(b, reinterpret_cast<f32x4_any4*>(p + 4));
+    } else {
+      *reinterpret_cast<f32x4_any4*>(p) = a;
+      *reinterpret_cast<f32x4_any4*>(p + 4) = b;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -94,17 +102,51 @@ __device__ inline void store_bytes(uint8_t* __restrict__ p, int64_t valid, i32x2
   }
 }
 
+// exp and log in FP64, to a few units of 2^-53, from their series: exp(r) with |r| <= ln(2) / 2 behind a power of two (thirteen terms: the first one
+// left out is below 2^-57), log(f) = 2 atanh((f - 1) / (f + 1)) with f in [sqrt(1/2), sqrt(2)] (|quotient| <= 0.172: eleven terms, 2^-60).  The
+// coefficients lie in memory, so that they are scalar operands: the library's functions, inlined into a loop, have theirs
+// kept in vector registers, which the kernels that hold a row there do not have (and a call would cost them as many).
+__constant__ double kExpSeries[14] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880,
+                                             1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600, 1.0 / 6227020800.0};
+__constant__ double kLogSeries[11] = {2.0, 2.0 / 3, 2.0 / 5, 2.0 / 7, 2.0 / 9, 2.0 / 11, 2.0 / 13, 2.0 / 15, 2.0 / 17, 2.0 / 19, 2.0 / 21};
+constexpr double kLn2 = 0.6931471805599453, kLn2Rest = 2.3190468138462996e-17, kLog2e = 1.4426950408889634;
+__device__ inline double exp_series(double x) {          // NaN stays NaN; beyond FP64's range 0 or infinity
+  x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;
+  const double n = __builtin_rint(x * kLog2e);
+  const double r = __builtin_fma(-n, kLn2Rest, __builtin_fma(-n, kLn2, x));
+  double p = kExpSeries[13];
+#pragma unroll
+  for (int i = 12; i >= 0; --i) p = __builtin_fma(p, r, kExpSeries[i]);
+  return __builtin_ldexp(p, (int)n);
+}
+__device__ inline double log_series(double x) {          // of a number that is not negative: 0 -> -infinity, infinity and NaN stay
+  int e;
+  double f = __builtin_frexp(x, &e);                     // [1/2, 1)
+  if (f < 0.7071067811865476) { f += f; --e; }
+  const double q = (f - 1.0) / (f + 1.0), q2 = q * q;
+  double p = kLogSeries[10];
+#pragma unroll
+  for (int i = 9; i >= 0; --i) p = __builtin_fma(p, q2, kLogSeries[i]);
+  p = __builtin_fma((double)e, kLn2, __builtin_fma(p, q, (double)e * kLn2Rest));
+  return x == 0.0 ? -__builtin_inf() : x < __builtin_inf() ? p : x;
+}
+
 template <class T> __device__ inline float load_one(const T* p, int64_t i);
 template <> __device__ inline float load_one<uint16_t>(const uint16_t* p, int64_t i) { return bf16_decode(p[i]); }
 template <> __device__ inline float load_one<float>(const float* p, int64_t i) { return p[i]; }
 __device__ inline void store_one(uint16_t* p, int64_t i, float f) { p[i] = (uint16_t)pack_bf16(f, f); }
 __device__ inline void store_one(float* p, int64_t i, float f) { p[i] = f; }
 
-// Reductions over a wave: every lane gets the result.
-template <class T, class Op> __device__ inline T wave_reduce(T v, Op op) {
+// Reductions over a wave, or over each N of its lanes: every lane gets the result.
+template <int N = 64, class T, class Op> __device__ inline T wave_reduce(T v, Op op) {
 #pragma unroll
-  for (int m = 32; m; m >>= 1) v = op(v, __shfl_xor(v, m));
+  for (int m = N / 2; m; m >>= 1) v = op(v, __shfl_xor(v, m));
   return v;
+}
+// The waves' results of a workgroup, one a wave in `slots` behind a barrier (a lane reads one of them: sixteen held at once cost a kernel
+// that is short of registers more than the exchange between lanes does).
+template <int NW, class T, class Op> __device__ inline T slots_reduce(const T* slots, int lane, Op op) {
+  return wave_reduce<NW>(slots[lane & (NW - 1)], op);
 }
 __device__ inline float wave_sum(float v) {
   return wave_reduce(v, [](float a, float b) { return a + b; });
