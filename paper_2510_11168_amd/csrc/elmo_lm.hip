@@ -211,9 +211,9 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
   while (((int64_t)1 << bits) < V) ++bits;
   const elmo::SampleArgs a{logits, logits_stride, V, u, temperature, top_p, min_p, top_k, idx_out, prob_out, std::min(50, 62 - bits)};
   hipStream_t st = (hipStream_t)hip_stream;
-  if (dtype == ELMO_BF16) elmo::k_sample_plain<uint16_t><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
-  else elmo::k_sample_plain<float><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
-  return check_launch("k_sample_plain");
+  if (dtype == ELMO_BF16) elmo::k_sample<uint16_t><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
+  else elmo::k_sample<float><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
+  return check_launch("k_sample");
 }
 
 namespace {
