@@ -164,6 +164,55 @@ extern "C" int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const v
   return check_launch("k_norm_dweight");
 }
 
+namespace {
+template <class O, int TM, int TN, int FM, int FN, int NST> int launch_int8_tiles(const elmo::Int8Args& p, hipStream_t st) {
+  constexpr int smem = elmo::int8_smem<TM, TN, NST>();
+  static_assert(smem <= 160 * 1024, "LDS of the tiles");
+  // once per process and instantiation, whichever host thread comes first
+  static std::once_flag once;
+  static hipError_t attr_rc = hipSuccess;
+  std::call_once(once, [] {
+    attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&elmo::k_int8_tiles<O, TM, TN, FM, FN, NST>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  });
+  if (attr_rc != hipSuccess) return fail(-3, "hipFuncSetAttribute(k_int8_tiles) failed: %s", hipGetErrorString(attr_rc));
+  const int tiles_m = (p.M + TM - 1) / TM, tiles_n = (p.N + TN - 1) / TN;
+  elmo::k_int8_tiles<O, TM, TN, FM, FN, NST><<<tiles_m * tiles_n, elmo::int8_threads<TM, TN, FM, FN>(), smem, st>>>(p, tiles_m, tiles_n);
+  return check_launch("k_int8_tiles");
+}
+template <class O, int FM> int launch_int8_skinny(const elmo::Int8Args& p, hipStream_t st) {
+  elmo::k_int8_skinny<O, FM><<<(unsigned)((p.N + 15) / 16), elmo::kSkinnyThreads, 0, st>>>(p);
+  return check_launch("k_int8_skinny");
+}
+// Which kernel (times in us, MI355X, BF16 outputs):
+//  - up to 16 tokens the kernel that streams the weights into registers, where its workgroups have K enough for their eight waves (1 x 4096 x 4096
+//    4.9, 64 x 64 tiles 12.4; 16 x 8192 x 8192 18.2 / 23.3) or are few; wide and short it loses (16 x 131072 x 768 33.0 / 23.2).  Up to 32 tokens it reads
+//    the tokens as often as that again and pays for one round of workgroups only (32 x 4096 x 4096 8.0 / 13.3; 32 x 32000 x 4096 46 / 23).
+//  - else tiles, by the time of the rounds in which they go over the 256 CUs at K = 4096: 256 x 256 63 a round of 256, 128 x 128 40 a round of 512 (two a
+//    CU; 26 if there are only 256), 64 x 64 18 a round of 512 (14).  8192 x 14336: 406 in tiles of 256, 502 of 128; 2048 x 4096: 50 / 41;
+//    512 x 4096: 42 / 22.5 / 18.8.
+//  - rows that are not 16-byte aligned, or of less than 128 bytes: 64 x 64 tiles through registers (8192 x 14336 x 4096: 1130).
+template <class O> int launch_int8(elmo::Int8Args p, hipStream_t st) {
+  if (p.M == 1) p.as = 0;                                  // (a single row's stride means nothing)
+  if (p.N == 1) p.bs = 0;
+  const auto tiles = [&](int t) { return (int64_t)((p.M + t - 1) / t) * ((p.N + t - 1) / t); };
+  const auto rounds = [](int64_t n, int64_t slots) { return (n + slots - 1) / slots; };
+  if (tiles(64) > kMostRows) return fail(-1, "M x N = %d x %d is more than one launch takes", p.M, p.N);
+  if (p.M <= 16 && (p.K >= 2048 || p.N <= 16384)) return launch_int8_skinny<O, 1>(p, st);
+  if (p.M <= 32 && p.N <= 4096) return launch_int8_skinny<O, 2>(p, st);
+  // (row offsets within a tile are formed from 24-bit factors)
+  const bool aligned = !(((uintptr_t)p.a | (uintptr_t)p.b | (uint64_t)p.as | (uint64_t)p.bs) & 15) && p.as < (1 << 24) && p.bs < (1 << 24);
+  if (!aligned || p.K < 128) {
+    elmo::k_int8_plain<O><<<(unsigned)tiles(64), elmo::kThreads, 0, st>>>(p);
+    return check_launch("k_int8_plain");
+  }
+  const int64_t t256 = 63 * rounds(tiles(256), 256), t128 = tiles(128) <= 256 ? 26 : 40 * rounds(tiles(128), 512),
+                t64 = tiles(64) <= 256 ? 14 : 18 * rounds(tiles(64), 512);
+  if (t256 <= t128 && t256 <= t64) return launch_int8_tiles<O, 256, 256, 2, 4, 2>(p, st);
+  if (t128 <= t64) return launch_int8_tiles<O, 128, 128, 1, 2, 2>(p, st);
+  return launch_int8_tiles<O, 64, 64, 1, 1, 4>(p, st);
+}
+}  // namespace
+
 extern "C" int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, const int8_t* b, int64_t b_stride, const float* b_scale,
                                 const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t out_stride, int out_dtype,
                                 void* hip_stream) {
@@ -181,12 +230,8 @@ extern "C" int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* 
   ELMO_TRY(check_aligned("bias", bias, ELMO_FP32));
   ELMO_TRY(check_aligned("out", out, out_dtype));
   const elmo::Int8Args p{(const char*)a, (const char*)b, a_scale, b_scale, bias, out, a_stride, b_stride, out_stride, (int)M, (int)N, (int)K};
-  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-  if (tiles > kMostRows) return fail(-1, "M x N = %lld x %lld is more than one launch takes", (long long)M, (long long)N);
   hipStream_t st = (hipStream_t)hip_stream;
-  if (out_dtype == ELMO_BF16) elmo::k_int8_plain<uint16_t><<<(unsigned)tiles, elmo::kThreads, 0, st>>>(p);
-  else elmo::k_int8_plain<float><<<(unsigned)tiles, elmo::kThreads, 0, st>>>(p);
-  return check_launch("k_int8_plain");
+  return out_dtype == ELMO_BF16 ? launch_int8<uint16_t>(p, st) : launch_int8<float>(p, st);
 }
 
 namespace {

@@ -73,9 +73,11 @@ __device__ inline void barrier_lds() {
 // whole tile rows; each lane fetches the global chunk that belongs at its swizzled position.
 // Rows at or beyond rows_valid (>= 1) re-read the last valid row.  Issues ROWS*ROWB/4096 loads per
 // wave; completion is tracked by vmcnt in issue order.
-template <int ROWS, int ROWB, int NW>
+// rows(r): the matrix's row that tile row r holds.
+struct SameRow { __device__ inline int operator()(int r) const { return r; } };
+template <int ROWS, int ROWB, int NW, class Rows = SameRow>
 __device__ inline void dma_tile(const char* __restrict__ g, size_t stride, int rows_valid, char* lds_tile, int wave, int lane,
-                                int chunks_valid = 1 << 20) {
+                                int chunks_valid = 1 << 20, Rows rows = Rows{}) {
   constexpr int RPI = 1024 / ROWB, CPR = ROWB / 16, NI = ROWS / RPI / NW;
   static_assert(ROWS % (RPI * NW) == 0 && NI >= 1, "tile must split evenly over the waves");
   // The slab pointer is wave-uniform.  Passing it through an empty asm statement as a scalar
@@ -91,7 +93,7 @@ __device__ inline void dma_tile(const char* __restrict__ g, size_t stride, int r
     const int rbase = (wave * NI + i) * RPI;
     const int r = rbase + lane / CPR;
     const int c = min((lane % CPR) ^ swz_key<ROWB>(r), chunks_valid - 1);   // chunks past a short row re-read its last one
-    const int rc = min(r, rows_valid - 1);
+    const int rc = min(rows(r), rows_valid - 1);
     // 32-bit lane offset on top of the (wave-uniform) slab pointer: the load then takes the
     // scalar-base + vector-offset form and needs no 64-bit address arithmetic per lane
     const uint32_t off = __umul24((uint32_t)rc, (uint32_t)stride) + (uint32_t)(c * 16);
