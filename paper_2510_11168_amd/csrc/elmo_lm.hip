@@ -165,19 +165,22 @@ extern "C" int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const v
 }
 
 namespace {
-template <class O, int TM, int TN, int FM, int FN, int NST> int launch_int8_tiles(const elmo::Int8Args& p, hipStream_t st) {
+template <class O, int TM, int TN, int FM, int FN, int NST, bool ASYNC> int launch_int8_as(const elmo::Int8Args& p, hipStream_t st) {
   constexpr int smem = elmo::int8_smem<TM, TN, NST>();
   static_assert(smem <= 160 * 1024, "LDS of the tiles");
   // once per process and instantiation, whichever host thread comes first
   static std::once_flag once;
   static hipError_t attr_rc = hipSuccess;
   std::call_once(once, [] {
-    attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&elmo::k_int8_tiles<O, TM, TN, FM, FN, NST>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&elmo::k_int8_tiles<O, TM, TN, FM, FN, NST, ASYNC>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (attr_rc != hipSuccess) return fail(-3, "hipFuncSetAttribute(k_int8_tiles) failed: %s", hipGetErrorString(attr_rc));
   const int tiles_m = (p.M + TM - 1) / TM, tiles_n = (p.N + TN - 1) / TN;
-  elmo::k_int8_tiles<O, TM, TN, FM, FN, NST><<<tiles_m * tiles_n, elmo::int8_threads<TM, TN, FM, FN>(), smem, st>>>(p, tiles_m, tiles_n);
+  elmo::k_int8_tiles<O, TM, TN, FM, FN, NST, ASYNC><<<tiles_m * tiles_n, elmo::int8_threads<TM, TN, FM, FN>(), smem, st>>>(p, tiles_m, tiles_n);
   return check_launch("k_int8_tiles");
+}
+template <class O, int TM, int TN, int FM, int FN, int NST> int launch_int8_tiles(const elmo::Int8Args& p, bool aligned, hipStream_t st) {
+  return aligned ? launch_int8_as<O, TM, TN, FM, FN, NST, true>(p, st) : launch_int8_as<O, TM, TN, FM, FN, 2, false>(p, st);
 }
 template <class O, int FM> int launch_int8_skinny(const elmo::Int8Args& p, hipStream_t st) {
   elmo::k_int8_skinny<O, FM><<<(unsigned)((p.N + 15) / 16), elmo::kSkinnyThreads, 0, st>>>(p);
@@ -190,7 +193,6 @@ template <class O, int FM> int launch_int8_skinny(const elmo::Int8Args& p, hipSt
 //  - else tiles, by the time of the rounds in which they go over the 256 CUs at K = 4096: 256 x 256 63 a round of 256, 128 x 128 40 a round of 512 (two a
 //    CU; 26 if there are only 256), 64 x 64 18 a round of 512 (14).  8192 x 14336: 406 in tiles of 256, 502 of 128; 2048 x 4096: 50 / 41;
 //    512 x 4096: 42 / 22.5 / 18.8.
-//  - rows that are not 16-byte aligned, or of less than 128 bytes: 64 x 64 tiles through registers (8192 x 14336 x 4096: 1130).
 template <class O> int launch_int8(elmo::Int8Args p, hipStream_t st) {
   if (p.M == 1) p.as = 0;                                  // (a single row's stride means nothing)
   if (p.N == 1) p.bs = 0;
@@ -201,15 +203,11 @@ template <class O> int launch_int8(elmo::Int8Args p, hipStream_t st) {
   if (p.M <= 32 && p.N <= 4096) return launch_int8_skinny<O, 2>(p, st);
   // (row offsets within a tile are formed from 24-bit factors)
   const bool aligned = !(((uintptr_t)p.a | (uintptr_t)p.b | (uint64_t)p.as | (uint64_t)p.bs) & 15) && p.as < (1 << 24) && p.bs < (1 << 24);
-  if (!aligned || p.K < 128) {
-    elmo::k_int8_plain<O><<<(unsigned)tiles(64), elmo::kThreads, 0, st>>>(p);
-    return check_launch("k_int8_plain");
-  }
   const int64_t t256 = 63 * rounds(tiles(256), 256), t128 = tiles(128) <= 256 ? 26 : 40 * rounds(tiles(128), 512),
                 t64 = tiles(64) <= 256 ? 14 : 18 * rounds(tiles(64), 512);
-  if (t256 <= t128 && t256 <= t64) return launch_int8_tiles<O, 256, 256, 2, 4, 2>(p, st);
-  if (t128 <= t64) return launch_int8_tiles<O, 128, 128, 1, 2, 2>(p, st);
-  return launch_int8_tiles<O, 64, 64, 1, 1, 4>(p, st);
+  if (t256 <= t128 && t256 <= t64) return launch_int8_tiles<O, 256, 256, 2, 4, 2>(p, aligned, st);
+  if (t128 <= t64) return launch_int8_tiles<O, 128, 128, 1, 2, 2>(p, aligned, st);
+  return launch_int8_tiles<O, 64, 64, 1, 1, 4>(p, aligned, st);
 }
 }  // namespace
 

@@ -30,43 +30,11 @@ template <class O> __device__ inline void store_out(const Int8Args& p, int m, in
   store_one((O*)p.out + (int64_t)m * p.os, n, p.bias ? v + p.bias[n] : v);
 }
 
-// 64 x 64 outputs a workgroup, 32 x 32 a wave; slabs of 64 bytes of K through LDS.
-constexpr int kInt8Row = 80;         // bytes of an LDS row: 64 of K, 16 of padding
-template <class O>
-__global__ __launch_bounds__(kThreads) void k_int8_plain(Int8Args p) {
-  __shared__ __align__(16) char sa[64 * kInt8Row], sb[64 * kInt8Row];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int tiles_n = (p.N + 63) / 64;
-  const int m0 = (int)(blockIdx.x / tiles_n) * 64, n0 = (int)(blockIdx.x % tiles_n) * 64;
-  const int r = tid >> 2, c = (tid & 3) * 16;
-  const char* a = p.a + (int64_t)min(m0 + r, p.M - 1) * p.as;
-  const char* b = p.b + (int64_t)min(n0 + r, p.N - 1) * p.bs;
-  const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-  i32x16 acc = {};
-  for (int k0 = 0; k0 < p.K; k0 += 64) {
-    *reinterpret_cast<i32x4*>(sa + r * kInt8Row + c) = load_k16(a, k0 + c, p.K);
-    *reinterpret_cast<i32x4*>(sb + r * kInt8Row + c) = load_k16(b, k0 + c, p.K);
-    __syncthreads();
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const int at = ks * 32 + 16 * (lane >> 5);
-      const i32x4 fa = *reinterpret_cast<const i32x4*>(sa + (wm + (lane & 31)) * kInt8Row + at);
-      const i32x4 fb = *reinterpret_cast<const i32x4*>(sb + (wn + (lane & 31)) * kInt8Row + at);
-      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa, fb, acc, 0, 0, 0);
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int m = m0 + wm + acc_row(v, lane), n = n0 + wn + (lane & 31);
-    if (m < p.M && n < p.N) store_out<O>(p, m, n, acc[v]);
-  }
-}
-
 // ---------------------------------------------------------------------------------------------
-// The product in tiles of TM x TN outputs (waves of 32 FM x 32 FN) over slabs of 128 bytes of K, for operands whose rows are 16-byte
-// aligned.  Slabs go to LDS by asynchronous loads, NST stages; as in ring_stream_pp half of the waves issue behind the barrier
+// The product in tiles of TM x TN outputs (waves of 32 FM x 32 FN) over slabs of 128 bytes of K.
+// ASYNC, for operands whose rows are 16-byte aligned: slabs go to LDS by asynchronous loads, NST stages; as in ring_stream_pp half of the waves issue behind the barrier
 // (all of A and half of B) and half in the middle of the slab, so that one wave of every SIMD multiplies while the other is held by its loads.
+// Otherwise a slab goes through registers, its loads in flight while the one before is multiplied, to the other of two stages.
 // v_mfma_i32_32x32x32_i8: lane i holds row i % 32 of an operand, 16 bytes of K from 16 (i / 32) on.
 // Tile row 32 j + l of a wave's columns holds weight row FN l + j: a lane then has FN neighbouring outputs of a row, and a wave stores 32 FN of them next
 // to each other.
@@ -112,7 +80,7 @@ template <class O, int FN> __device__ inline void store_columns(O* p, int valid,
   }
 }
 
-template <class O, int TM, int TN, int FM, int FN, int NST>
+template <class O, int TM, int TN, int FM, int FN, int NST, bool ASYNC>
 __global__ __launch_bounds__((int8_threads<TM, TN, FM, FN>())) void k_int8_tiles(Int8Args p, int tiles_m, int tiles_n) {
   constexpr int NT = int8_threads<TM, TN, FM, FN>(), NH = NT / 128, WGN = TN / 32 / FN, ABYTES = TM * 128, SBYTES = ABYTES + TN * 128, BH = TN / 2;
   constexpr int LPS_LATE = dma_loads_per_wave<BH, 128, NH>(), LPS_EARLY = dma_loads_per_wave<TM, 128, NH>() + LPS_LATE;
@@ -150,6 +118,15 @@ __global__ __launch_bounds__((int8_threads<TM, TN, FM, FN>())) void k_int8_tiles
     }
   };
   const int nk = p.K >> 7;
+  // chunk id of a slab: tile row, place in it, and its row of the operand
+  const auto chunk_row = [&](int id) {
+    const int r = id >> 3;
+    return r < TM ? a + (int64_t)min(r, mv - 1) * p.as : b + (int64_t)min(Interleave<FN>{}(r - TM), nv - 1) * p.bs;
+  };
+  const auto chunk_at = [&](int id) {
+    const int r = id >> 3, c = id & 7;
+    return r < TM ? tile_off<128>(r, c) : ABYTES + tile_off<128>(r - TM, c);
+  };
   const auto run = [&](const char* __restrict__ ga, const char* __restrict__ gb, char* __restrict__ ring) {
     const auto issue = [&](int ks) {
       char* st = ring + (ks % NST) * SBYTES;
@@ -178,17 +155,42 @@ __global__ __launch_bounds__((int8_threads<TM, TN, FM, FN>())) void k_int8_tiles
       half_slab(st, st + ABYTES, 1);
     }
   };
-  run(a, b, smem);
+  if constexpr (ASYNC) {
+    run(a, b, smem);
+  } else {
+    static_assert(NST == 2, "two stages");
+    constexpr int NC = (TM + TN) * 8 / NT;
+    const char* row[NC];
+    i32x4 v[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) row[i] = chunk_row(i * NT + tid) + 16 * (tid & 7);
+    const auto fetch = [&](int ks) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] = *reinterpret_cast<const i32x4_any1*>(row[i] + (size_t)ks * 128);
+    };
+    const auto lay = [&](int ks) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) *reinterpret_cast<i32x4*>(smem + (ks & 1) * SBYTES + chunk_at(i * NT + tid)) = v[i];
+    };
+    if (nk > 0) {
+      fetch(0);
+      lay(0);
+    }
+    for (int ks = 0; ks < nk; ++ks) {
+      barrier_lds();
+      if (ks + 1 < nk) fetch(ks + 1);
+      const char* st = smem + (ks & 1) * SBYTES;
+      half_slab(st, st + ABYTES, 0);
+      half_slab(st, st + ABYTES, 1);
+      if (ks + 1 < nk) lay(ks + 1);                        // (its stage was last read before this round's barrier)
+    }
+  }
   __syncthreads();
   // the last K % 128 bytes through registers, zeros behind them; the scales beside them
   if (p.K & 127) {
 #pragma unroll 1
-    for (int id = tid; id < (TM + TN) * 8; id += NT) {
-      const int r = id >> 3, c = id & 7;
-      const bool of_a = r < TM;
-      const char* row = of_a ? a + (int64_t)min(r, mv - 1) * p.as : b + (int64_t)min(Interleave<FN>{}(r - TM), nv - 1) * p.bs;
-      *reinterpret_cast<i32x4*>(smem + (of_a ? tile_off<128>(r, c) : ABYTES + tile_off<128>(r - TM, c))) = load_k16(row, nk * 128 + 16 * c, p.K);
-    }
+    for (int id = tid; id < (TM + TN) * 8; id += NT)
+      *reinterpret_cast<i32x4*>(smem + chunk_at(id)) = load_k16(chunk_row(id), nk * 128 + 16 * (id & 7), p.K);
   }
   for (int i = tid; i < TM; i += NT) s_sa[i] = p.sa[m0 + min(i, mv - 1)];
   for (int i = tid; i < TN; i += NT) {
