@@ -228,6 +228,10 @@ _ROWS = {**_REAL, torch.float8_e4m3fn: ELMO_FP8_E4M3, torch.uint8: ELMO_FP8_E4M3
 _ONLY_FP32, _ONLY_INT32, _ONLY_INT8 = {torch.float32: ELMO_FP32}, {torch.int32: 0}, {torch.int8: ELMO_INT8}
 
 
+_SAME = {code: {t: c for t, c in _REAL.items() if c == code} for code in (ELMO_BF16, ELMO_FP32)}     # the types of one code
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # current_stream() without its Python object, a few us less of a small call
+
+
 def _matrix(name, t, types, rows=None, cols=None):
     """(address, row stride, type code) of a 2-D tensor whose rows are dense; (None, 0, 0) for None."""
     if t is None:
@@ -235,10 +239,11 @@ def _matrix(name, t, types, rows=None, cols=None):
     code = types.get(t.dtype)
     if code is None:
         raise ElmoError(-2, f"{name}: unsupported dtype {t.dtype}")
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ElmoError(-1, f"{name}: shape {tuple(t.shape)}, expected ({'rows' if rows is None else rows}, {'columns' if cols is None else cols})")
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise ElmoError(-1, f"{name}: shape {tuple(shape)}, expected ({'rows' if rows is None else rows}, {'columns' if cols is None else cols})")
     stride, step = t.stride()
-    if step != 1 and t.shape[1] > 1:
+    if step != 1 and shape[1] > 1:
         raise ElmoError(-1, f"{name}: the elements of a row must lie next to each other (stride {step})")
     return t.data_ptr(), stride, code
 
@@ -250,7 +255,7 @@ def _vector(name, t, types, n):
     code = types.get(t.dtype)
     if code is None:
         raise ElmoError(-2, f"{name}: unsupported dtype {t.dtype}")
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.shape != (n,) or not t.is_contiguous():
         raise ElmoError(-1, f"{name}: shape {tuple(t.shape)} with strides {t.stride()}, expected {n} dense elements")
     return t.data_ptr(), code
 
@@ -263,26 +268,32 @@ def _needed(**tensors):
 
 def _call(fn, args, tensors, stream, workspace=None, bytes_needed=None):
     """fn(*args[, workspace, its size], stream) on the device that holds all `tensors`."""
-    device = tensors[0].device
+    index = tensors[0].get_device()         # -1: not on a GPU
     for t in tensors:
-        if t is not None and t.device != device:
-            raise ElmoError(-1, f"tensors on {t.device} and {device}")
-    if device.type != "cuda":
-        raise ElmoError(-1, f"the tensors must be on the GPU (got {device})")
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
+        if t is not None and t.get_device() != index:
+            raise ElmoError(-1, f"tensors on {t.device} and {tensors[0].device}")
+    if index < 0:
+        raise ElmoError(-1, f"the tensors must be on the GPU (got {tensors[0].device})")
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
             return _call(fn, args, tensors, stream, workspace, bytes_needed)
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is not None:
+        if stream.device.index != index:
+            raise ElmoError(-1, f"stream of {stream.device}, tensors on {tensors[0].device}")
+        handle = stream.cuda_stream
+    else:
+        handle = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
     if bytes_needed is None:
-        return _check(fn(*args, stream.cuda_stream))
-    if workspace is None and bytes_needed:
+        return _check(fn(*args, handle))
+    if workspace is not None:
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise ElmoError(-1, f"workspace: a dense tensor on {tensors[0].device} is needed")
+    elif bytes_needed and stream is None:
+        workspace = torch.empty(bytes_needed, dtype=torch.uint8, device=tensors[0].device)
+    elif bytes_needed:
         with torch.cuda.stream(stream):     # the caching allocator then reuses it in this stream's order
-            workspace = torch.empty(bytes_needed, dtype=torch.uint8, device=device)
-    elif workspace is not None:
-        if workspace.device != device or not workspace.is_contiguous():
-            raise ElmoError(-1, f"workspace: a dense tensor on {device} is needed")
-    return _check(fn(*args, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), stream.cuda_stream))
+            workspace = torch.empty(bytes_needed, dtype=torch.uint8, device=tensors[0].device)
+    return _check(fn(*args, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), handle))
 
 
 def elmo_rms_norm(x, y, weight=None, eps=1e-6, *, residual=None, sum_out=None, scale_out=None, stream=None) -> None:
@@ -290,7 +301,7 @@ def elmo_rms_norm(x, y, weight=None, eps=1e-6, *, residual=None, sum_out=None, s
     _needed(x=x, y=y)
     xp, xs, dtype = _matrix("x", x, _REAL)
     rows, d = x.shape
-    real = {k: v for k, v in _REAL.items() if v == dtype}
+    real = _SAME[dtype]
     rp, rs, _ = _matrix("residual", residual, real, rows, d)
     sp, ss, _ = _matrix("sum_out", sum_out, real, rows, d)
     yp, ys, yt = _matrix("y", y, _ROWS, rows, d)
@@ -309,7 +320,7 @@ def elmo_rms_norm_backward(dy, h, dh, weight=None, eps=1e-6, *, dsum=None, dweig
     _needed(dy=dy, h=h, dh=dh)
     yp, ys, dtype = _matrix("dy", dy, _REAL)
     rows, d = dy.shape
-    real = {k: v for k, v in _REAL.items() if v == dtype}
+    real = _SAME[dtype]
     hp, hs, _ = _matrix("h", h, real, rows, d)
     op, os_, _ = _matrix("dh", dh, real, rows, d)
     sp, ss, _ = _matrix("dsum", dsum, real, rows, d)
@@ -368,7 +379,7 @@ def elmo_distill(logits, teacher_idx, teacher_logits, loss_out, grad_out=None, *
     lp, ls, lt = _matrix("teacher_logits", teacher_logits, _REAL, rows, K)
     if rows > 1 and (ts != K or ls != K):
         raise ElmoError(-1, "teacher_idx and teacher_logits must be dense")
-    gp, gs, _ = _matrix("grad_out", grad_out, {k: v for k, v in _REAL.items() if v == dtype}, rows, V)
+    gp, gs, _ = _matrix("grad_out", grad_out, _SAME[dtype], rows, V)
     op, _ = _vector("loss_out", loss_out, _ONLY_FP32, rows)
     vp, _ = _vector("row_weight", row_weight, _ONLY_FP32, rows)
     _call(_lib.elmo_distill, (zp, zs, dtype, rows, V, tp, lp, lt, K, temperature, vp, op, gp, gs),

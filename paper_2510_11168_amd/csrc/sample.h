@@ -128,6 +128,30 @@ __device__ inline void sort_falling(uint64_t* s, int n, int tid) {
   __syncthreads();
 }
 
+// The list in falling order, s_list[0, n) with n <= kSampleCount: every place's rank is the number of larger ones, counted by as many threads as there are
+// for it (64 places: 0.3 us; the exchanges of a sort are a barrier each).  `rank` has kSampleCount entries.  Barriers before and behind.
+constexpr int kSampleCount = 256;
+template <class F> __device__ inline void for_pairs(int n, int tid, F&& f) {     // f(i, a stretch [from, to) of the others), all of them once
+  int size = 1;
+  while (size < n) size *= 2;
+  const int i = tid & (size - 1), parts = kSampleThreads / size, per = (n + parts - 1) / parts, from = tid / size * per;
+  if (i < n && from < n) f(i, from, min(n, from + per));
+}
+__device__ inline void rank_falling(uint64_t* list, uint32_t* rank, int n, int tid) {
+  if (tid < kSampleCount) rank[tid] = 0;
+  __syncthreads();
+  const uint64_t mine = tid < n ? list[tid] : 0;
+  for_pairs(n, tid, [&](int i, int from, int to) {
+    const uint64_t x = list[i];
+    uint32_t larger = 0;
+    for (int j = from; j < to; ++j) larger += list[j] > x;
+    if (larger) atomicAdd(&rank[i], larger);
+  });
+  __syncthreads();
+  if (tid < n) list[rank[tid]] = mine;
+  __syncthreads();
+}
+
 template <class T>
 __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
   constexpr int NT = kSampleThreads;
@@ -156,7 +180,7 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
   // ---- largest logit, and each thread's
   if (tid < 256) s_root[tid] = exp_series(tid * (kLn2 / 256));
   float mine = -__builtin_inff();
-#pragma unroll 4
+#pragma unroll 8
   for (int64_t o = tid; o < octets; o += NT) {
     float f[8];
     load8(o, f);
@@ -186,7 +210,7 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
   float low = -__builtin_inff();                         // no kept logit lies below this
   // appends what keep(logit, octet's first index + i) names among the octets whose largest logit is at least `from` to the list
   const auto collect = [&](float from, auto&& keep) {
-#pragma unroll 2
+#pragma unroll 4
     for (int64_t o = tid; o < octets; o += NT) {
       float f[8];
       load8(o, f);
@@ -260,27 +284,41 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
     collect(from, [](float f) { return f > -__builtin_inff(); });
     const int n = s_n;
     if (n <= kSampleList) {
-      pad_and_sort(n);
+      if (n <= kSampleCount) rank_falling(s_list, s_count, n, tid);
+      else pad_and_sort(n);
       const int nk = (int)min((int64_t)n, rs.k);         // at most 512: one a thread
       const uint64_t place = tid < nk ? s_list[tid] : 0, w = tid < nk ? weigh(of_key(place >> 32)) : 0;
       uint64_t total;
       const uint64_t upto = block_scan(w, s_sum, wave, lane, total);
       const bool kept = w >= least && (rs.p >= 1.0 || upto - w < share_of(rs.p, total));
-      // by index: the kept ones' complements of the index above their weights' places
-      if (tid < kSampleShortK) {
-        s_mass[tid] = w;
-        s_list[tid] = kept ? place << 32 | (uint32_t)tid : 0;
-      }
-      int size = 2;
-      while (size < nk) size *= 2;
-      sort_falling(s_list, size, tid);
-      const uint64_t entry = tid < size ? s_list[tid] : 0;
-      // (an entry of 0 would be index 2^32 - 1, which no row has)
-      const uint64_t wi = entry ? s_mass[(uint32_t)entry] : 0;
       uint64_t all;
-      const uint64_t by_index = block_scan(wi, s_sum, wave, lane, all);
+      block_scan(kept ? w : 0, s_sum, wave, lane, all);
       uint64_t want = (uint64_t)(rs.u * (double)all);
       if (want >= all) want = all - 1;
+      // what is kept before a token by index: of few by pairs, else along the list sorted by index
+      if (tid < kSampleShortK) {
+        s_mass[tid] = kept ? w : 0;
+        s_mass[kSampleShortK + tid] = 0;
+        if (nk > kSampleCount) s_list[tid] = kept ? place << 32 | (uint32_t)tid : 0;
+      }
+      __syncthreads();
+      if (nk <= kSampleCount) {
+        for_pairs(nk, tid, [&](int i, int from, int to) {
+          const uint32_t x = (uint32_t)s_list[i];        // the complement of the index
+          uint64_t sum = 0;
+          for (int j = from; j < to; ++j) sum += (uint32_t)s_list[j] > x ? s_mass[j] : 0;
+          if (sum) atomicAdd((unsigned long long*)&s_mass[kSampleShortK + i], (unsigned long long)sum);
+        });
+        __syncthreads();
+        const uint64_t before = tid < nk ? s_mass[kSampleShortK + tid] : 0;
+        if (kept && before <= want && before + w > want) answer((int64_t)(uint32_t)~(uint32_t)place, (float)((double)w / (double)all));
+        return;
+      }
+      sort_falling(s_list, kSampleShortK, tid);
+      const uint64_t entry = tid < kSampleShortK ? s_list[tid] : 0;
+      // (an entry of 0 would be index 2^32 - 1, which no row has)
+      const uint64_t wi = entry ? s_mass[(uint32_t)entry] : 0;
+      const uint64_t by_index = block_scan(wi, s_sum, wave, lane, all);
       if (wi && by_index > want && by_index - wi <= want) answer((int64_t)(uint32_t)~(uint32_t)(entry >> 32), (float)((double)wi / (double)all));
       return;
     }
