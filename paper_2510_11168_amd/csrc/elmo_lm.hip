@@ -236,7 +236,34 @@ namespace {
 constexpr int64_t kMostV = ((int64_t)1 << 31) - 1;
 }
 
-extern "C" size_t elmo_sample_bytes(int64_t rows, int64_t V) { return 0; }
+namespace {
+// Workgroups of a row without top-k: one where the rows fill the chip or are short.
+int sample_parts(int64_t rows, int64_t V) {
+  if (rows > 128 || V < 16384) return 1;
+  return (int)std::min<int64_t>(std::min<int64_t>(64, (V + 4095) / 4096), std::max<int64_t>(2, 256 / rows));
+}
+template <class T> int launch_sample(const elmo::SampleArgs& a, int64_t rows, hipStream_t st) {
+  const unsigned one = (unsigned)rows, all = (unsigned)(rows * a.parts);
+  if (a.parts == 1) {
+    elmo::k_sample<T, elmo::SAMPLE_WHOLE><<<one, elmo::kSampleThreads, 0, st>>>(a);
+    return check_launch("k_sample");
+  }
+  elmo::k_sample<T, elmo::SAMPLE_MAX><<<all, elmo::kSampleThreads, 0, st>>>(a);
+  ELMO_TRY(check_launch("k_sample (maxima)"));
+  if (a.top_p) {
+    elmo::k_sample<T, elmo::SAMPLE_BINS><<<all, elmo::kSampleThreads, 0, st>>>(a);
+    ELMO_TRY(check_launch("k_sample (bins)"));
+  }
+  elmo::k_sample<T, elmo::SAMPLE_SUMS><<<all, elmo::kSampleThreads, 0, st>>>(a);
+  ELMO_TRY(check_launch("k_sample (sums)"));
+  elmo::k_sample<T, elmo::SAMPLE_DRAW><<<one, elmo::kSampleThreads, 0, st>>>(a);
+  return check_launch("k_sample (draw)");
+}
+}  // namespace
+
+extern "C" size_t elmo_sample_bytes(int64_t rows, int64_t V) {
+  return rows < 1 || V < 1 || sample_parts(rows, V) == 1 ? 0 : (size_t)rows * elmo::kSampleRowBytes;
+}
 
 extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const float* u, const float* temperature,
                            const int32_t* top_k, const float* top_p, const float* min_p, int32_t* idx_out, float* prob_out, void* workspace,
@@ -252,11 +279,13 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
     ELMO_TRY(check_aligned("u, temperature, top_k, top_p, min_p, idx_out and prob_out", p, ELMO_FP32));
   int bits = 0;
   while (((int64_t)1 << bits) < V) ++bits;
-  const elmo::SampleArgs a{logits, logits_stride, V, u, temperature, top_p, min_p, top_k, idx_out, prob_out, std::min(50, 62 - bits)};
+  const size_t need = elmo_sample_bytes(rows, V);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return fail(-1, "workspace missing, smaller than %zu bytes or not 256-byte aligned", need);
+  // (with top-k the few tokens that stay are found faster by one workgroup)
+  const elmo::SampleArgs a{logits, logits_stride, V, u, temperature, top_p, min_p, top_k, idx_out, prob_out, std::min(50, 62 - bits),
+                           top_k ? 1 : sample_parts(rows, V), (char*)workspace};
   hipStream_t st = (hipStream_t)hip_stream;
-  if (dtype == ELMO_BF16) elmo::k_sample<uint16_t><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
-  else elmo::k_sample<float><<<(unsigned)rows, elmo::kSampleThreads, 0, st>>>(a);
-  return check_launch("k_sample");
+  return dtype == ELMO_BF16 ? launch_sample<uint16_t>(a, rows, st) : launch_sample<float>(a, rows, st);
 }
 
 namespace {

@@ -13,7 +13,9 @@
 //                  which is sorted, filtered and drawn from: two readings, no weights but the list's;
 //   top_p, top_k   counts and weights over bins of 1/32 octave of weight, then the tokens of the bin in which the filter ends, sorted (a bin
 //                  that holds too many: a radix search over their places); three readings, four with both;
-//   always         sums of the kept weights over segments of the row, and the token inside the segment on which the number falls.
+//   otherwise      sums of the kept weights over segments of the row, and the token inside the segment on which the number falls.
+// Few long rows without top-k go over several workgroups each, in four launches: maxima; bins; sums of the segments without the bin in which top-p ends,
+// whose tokens go to a list; and by one workgroup the list, its kept tokens added to their segments, and the draw.
 #pragma once
 #include "rows.h"
 
@@ -33,6 +35,8 @@ struct SampleArgs {
   int32_t* token;
   float* prob;
   int F;
+  int parts;                         // workgroups of a row
+  char* ws;                          // of split rows: kSampleRowBytes each
 };
 
 // Rises with the logit; -0 counts as +0, NaN as -infinity.
@@ -152,22 +156,42 @@ __device__ inline void rank_falling(uint64_t* list, uint32_t* rank, int n, int t
   __syncthreads();
 }
 
-template <class T>
-__global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
-  constexpr int NT = kSampleThreads;
-  __shared__ uint64_t s_list[kSampleList], s_mass[kSampleBins], s_sum[kSampleWaves];
-  __shared__ uint32_t s_count[kSampleBins], s_sum32[kSampleWaves];
-  __shared__ double s_root[256];
-  __shared__ float s_max[kSampleWaves];
-  __shared__ uint64_t s_found[3];
-  __shared__ int s_n;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = blockIdx.x, octets = (a.V + 7) >> 3;
-  const T* z = (const T*)a.z + row * a.zs;
-  const RowSettings rs = settings_of(a, row);
-  // an octet's logits; beyond the row -infinity.  Where the largest is +infinity only that has a weight: 0 stands for it, -infinity for the others.
-  bool infinite = false;
-  const auto load8 = [&](int64_t o, float (&f)[8]) {
+struct SampleLds {
+  uint64_t list[kSampleList], mass[kSampleBins], sum[kSampleWaves], found[3];
+  double root[256];
+  uint32_t count[kSampleBins], sum32[kSampleWaves];
+  float max[kSampleWaves];
+  int n;
+};
+
+// What a split row's workgroups hand on.
+struct SampleWs {
+  uint64_t mass[kSampleBins], list[kSampleList], segment[kSampleList];
+  float max[64];
+  uint32_t n;
+};
+constexpr size_t kSampleRowBytes = (sizeof(SampleWs) + 255) / 256 * 256;
+
+// One row in the hands of a workgroup.
+template <class T> struct Sampler {
+  static constexpr int NT = kSampleThreads;
+  const SampleArgs& a;
+  SampleLds& l;
+  const int64_t row, octets, per;              // per: rounds of 64 octets in a segment, which is a wave's
+  const int segments, tid, lane, wave;
+  const T* z;
+  const RowSettings rs;
+  bool infinite = false;                       // the largest logit is +infinity: only such have a weight; 0 stands for it, -infinity for the others
+  Weigh weigh;
+  uint64_t least = 1, edge = (uint64_t)(kKeyNone + 1) << 32;     // smallest kept weight; kept: places from here on
+  float low = -__builtin_inff();                                 // no kept logit lies below this
+
+  __device__ inline Sampler(const SampleArgs& args, SampleLds& lds, int64_t r)
+      : a(args), l(lds), row(r), octets((args.V + 7) >> 3), per(((octets + 63) / 64 + kSampleList - 1) / kSampleList),
+        segments((int)(((octets + 63) / 64 + per - 1) / per)), tid(threadIdx.x), lane(threadIdx.x & 63), wave(threadIdx.x >> 6),
+        z((const T*)args.z + r * args.zs), rs(settings_of(args, r)) {}
+
+  __device__ inline void load8(int64_t o, float (&f)[8]) const {
     const Octet<T> oc = load_octet(z + o * 8, a.V - o * 8, lowest<T>());
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = oc[i];
@@ -175,41 +199,40 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = f[i] == __builtin_inff() ? 0.0f : -__builtin_inff();
     }
-  };
-  const auto max8 = [](const float (&f)[8]) { return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7]))); };
-  // ---- largest logit, and each thread's
-  if (tid < 256) s_root[tid] = exp_series(tid * (kLn2 / 256));
-  float mine = -__builtin_inff();
-#pragma unroll 8
-  for (int64_t o = tid; o < octets; o += NT) {
-    float f[8];
-    load8(o, f);
-    mine = fmaxf(mine, max8(f));
   }
-  float M = wave_max(mine);
-  if (lane == 0) s_max[wave] = M;
-  if (tid == 0) s_n = 0;
-  __syncthreads();
-  M = slots_reduce<kSampleWaves>(s_max, lane, [](float p, float q) { return fmaxf(p, q); });
-  const auto answer = [&](int64_t token, float prob) {
+  static __device__ inline float max8(const float (&f)[8]) {
+    return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+  }
+  __device__ inline void answer(int64_t token, float prob) const {
     a.token[row] = (int32_t)token;
     if (a.prob) a.prob[row] = prob;
-  };
-  if (M == -__builtin_inff()) {
-    if (tid == 0) answer(-1, 0.0f);
-    return;
   }
-  if (M == __builtin_inff()) {
-    infinite = true;
-    M = 0.0f;
-    mine = mine == __builtin_inff() ? 0.0f : -__builtin_inff();
+  __device__ inline uint64_t number(uint64_t all) const {        // u of the kept weight
+    const uint64_t want = (uint64_t)(rs.u * (double)all);
+    return want >= all ? all - 1 : want;
   }
-  const Weigh weigh{s_root, (double)M, 256.0 * kLog2e / rs.t, -256.0 * (a.F + 2), a.F};
-  const uint64_t one = 1ull << a.F, least = rs.mp > 0.0 ? share_of(rs.mp, one) : 1;
-  uint64_t edge = (uint64_t)(kKeyNone + 1) << 32;        // kept: places from here on
-  float low = -__builtin_inff();                         // no kept logit lies below this
-  // appends what keep(logit, octet's first index + i) names among the octets whose largest logit is at least `from` to the list
-  const auto collect = [&](float from, auto&& keep) {
+  // A thread's largest logit among the octets [from, to).
+  __device__ inline float largest(int64_t from, int64_t to) const {
+    float m = -__builtin_inff();
+#pragma unroll 8
+    for (int64_t o = from + tid; o < to; o += NT) {
+      float f[8];
+      load8(o, f);
+      m = fmaxf(m, max8(f));
+    }
+    return m;
+  }
+  // The row's weights, once its largest logit is known (> -infinity).  Holds a barrier.
+  __device__ inline void set_max(float M) {
+    infinite = M == __builtin_inff();
+    if (tid < 256) l.root[tid] = exp_series(tid * (kLn2 / 256));
+    if (tid == 0) l.n = 0;
+    weigh = Weigh{l.root, infinite ? 0.0 : (double)M, 256.0 * kLog2e / rs.t, -256.0 * (a.F + 2), a.F};
+    if (rs.mp > 0.0) least = share_of(rs.mp, 1ull << a.F);
+    __syncthreads();
+  }
+  // Appends the logits >= from that keep() names to the list.
+  template <class F> __device__ inline void collect(float from, F&& keep) {
 #pragma unroll 4
     for (int64_t o = tid; o < octets; o += NT) {
       float f[8];
@@ -218,55 +241,53 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (f[i] >= from && keep(f[i])) {
-            const int at = atomicAdd(&s_n, 1);
-            if (at < kSampleList) s_list[at] = place_of(f[i], o * 8 + i);
+            const int at = atomicAdd(&l.n, 1);
+            if (at < kSampleList) l.list[at] = place_of(f[i], o * 8 + i);
           }
       }
     }
     __syncthreads();
-  };
-  const auto pad_and_sort = [&](int n) {                 // the list, to the next power of two
+  }
+  __device__ inline void order_list(int n) {
+    if (n <= kSampleCount) return rank_falling(l.list, l.count, n, tid);
     int size = 2;
     while (size < n) size *= 2;
-    for (int i = n + tid; i < size; i += NT) s_list[i] = 0;
-    sort_falling(s_list, size, tid);
-  };
-
-  if (rs.k <= kSampleShortK) {
-    // ---- few tokens stay: bound, list, sort, filter, draw
-    float from = M;
-    if (rs.k > 1) {
-      // 16 bits of the k-th largest of the threads' maxima, 8 at a time
-      uint32_t prefix = 0, left = (uint32_t)rs.k;
-      const uint32_t key = key_of(mine);
-      for (int sh = 24; sh >= 16; sh -= 8) {
-        if (tid < 256) s_count[tid] = 0;
-        __syncthreads();
-        if (key > kKeyNone && (sh == 24 || key >> 24 == prefix >> 24)) atomicAdd(&s_count[(key >> sh) & 255], 1u);
-        __syncthreads();
-        if (wave == 0) {                                 // four bins a lane, the largest first
-          uint32_t c[4], sum = 0;
+    for (int i = n + tid; i < size; i += NT) l.list[i] = 0;
+    sort_falling(l.list, size, tid);
+  }
+  // found[0] = the place at which the list's n tokens, behind `above` tokens of weight mass_above, first make up `want` tokens or weight; found[1]
+  // = the weight down to it.  Changes count.
+  __device__ inline void cut_list(int n, bool by_mass, uint64_t want, uint64_t above, uint64_t mass_above) {
+    order_list(n);
+    uint64_t w[4], sum = 0, whole;                       // four a thread
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sum += c[i] = s_count[255 - 4 * lane - i];
-          uint32_t before = wave_scan(sum, lane) - sum;
-          if (lane == 63) s_found[0] = before + sum < left ? ~0ull : 0;      // fewer maxima than k: every token is taken
+    for (int i = 0; i < 4; ++i) sum += w[i] = 4 * tid + i < n ? weigh(of_key(l.list[4 * tid + i] >> 32)) : 0;
+    uint64_t upto = mass_above + block_scan(sum, l.sum, wave, lane, whole) - sum;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (before < left && before + c[i] >= left) { s_found[1] = 255 - 4 * lane - i; s_found[2] = before; }
-            before += c[i];
-          }
-        }
-        __syncthreads();
-        if (s_found[0]) { prefix = 0; break; }
-        prefix |= (uint32_t)s_found[1] << sh;
-        left -= (uint32_t)s_found[2];
-        __syncthreads();
-      }
-      from = of_key(max(prefix, kKeyNone + 1));
+    for (int i = 0; i < 4; ++i) {
+      const int at = 4 * tid + i;
+      const bool here = at < n && (by_mass ? upto < want && upto + w[i] >= want : above + at + 1 == want);
+      upto += w[i];
+      if (here) { l.found[0] = l.list[at]; l.found[1] = upto; }
     }
+    __syncthreads();
+  }
+  // Into found: the bin in which tokens or weight, `before` ahead of this thread's two bins with c0 and c1, first make up `want`; what lies ahead of it; the
+  // weight ahead of it.
+  __device__ inline void find_bin(uint64_t want, uint64_t before, uint64_t c0, uint64_t c1, uint64_t mass_before, uint64_t m0) {
+    __syncthreads();
+    if (before < want && before + c0 >= want) { l.found[0] = 2 * tid; l.found[1] = before; l.found[2] = mass_before; }
+    if (before + c0 < want && before + c0 + c1 >= want) { l.found[0] = 2 * tid + 1; l.found[1] = before + c0; l.found[2] = mass_before + m0; }
+    __syncthreads();
+  }
+  // A bound below a bin's logits, with room for the rounding of y, so that octets below it are passed over.
+  __device__ inline float bin_floor(int bin) const { return (float)(weigh.M + (-8.0 * bin - 9.0) / weigh.k) - 1e-5f * fabsf((float)weigh.M); }
+
+  // ---- top_k <= 512: bound, list, filters, draw.  False: the list does not hold what lies above the bound.
+  __device__ inline bool short_list(float mine) {
+    const float M = (float)weigh.M;
     if (rs.k == 1) {
-      // the largest logit's first place
-      uint32_t first = ~0u;
+      uint32_t first = ~0u;                              // the largest logit's first place
       for (int64_t o = tid; o < octets; o += NT) {
         float f[8];
         load8(o, f);
@@ -275,66 +296,86 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
           if (f[i] == M) first = min(first, (uint32_t)(o * 8 + i));
       }
       first = wave_reduce(first, [](uint32_t p, uint32_t q) { return min(p, q); });
-      if (lane == 0) s_sum32[wave] = first;
+      if (lane == 0) l.sum32[wave] = first;
       __syncthreads();
-      first = slots_reduce<kSampleWaves>(s_sum32, lane, [](uint32_t p, uint32_t q) { return min(p, q); });
+      first = slots_reduce<kSampleWaves>(l.sum32, lane, [](uint32_t p, uint32_t q) { return min(p, q); });
       if (tid == 0) answer(first, 1.0f);
-      return;
+      return true;
     }
-    collect(from, [](float f) { return f > -__builtin_inff(); });
-    const int n = s_n;
-    if (n <= kSampleList) {
-      if (n <= kSampleCount) rank_falling(s_list, s_count, n, tid);
-      else pad_and_sort(n);
-      const int nk = (int)min((int64_t)n, rs.k);         // at most 512: one a thread
-      const uint64_t place = tid < nk ? s_list[tid] : 0, w = tid < nk ? weigh(of_key(place >> 32)) : 0;
-      uint64_t total;
-      const uint64_t upto = block_scan(w, s_sum, wave, lane, total);
-      const bool kept = w >= least && (rs.p >= 1.0 || upto - w < share_of(rs.p, total));
-      uint64_t all;
-      block_scan(kept ? w : 0, s_sum, wave, lane, all);
-      uint64_t want = (uint64_t)(rs.u * (double)all);
-      if (want >= all) want = all - 1;
-      // what is kept before a token by index: of few by pairs, else along the list sorted by index
-      if (tid < kSampleShortK) {
-        s_mass[tid] = kept ? w : 0;
-        s_mass[kSampleShortK + tid] = 0;
-        if (nk > kSampleCount) s_list[tid] = kept ? place << 32 | (uint32_t)tid : 0;
+    // 16 bits of the k-th largest of the threads' maxima, 8 at a time
+    uint32_t prefix = 0, left = (uint32_t)rs.k;
+    const uint32_t key = key_of(mine);
+    for (int sh = 24; sh >= 16; sh -= 8) {
+      if (tid < 256) l.count[tid] = 0;
+      __syncthreads();
+      if (key > kKeyNone && (sh == 24 || key >> 24 == prefix >> 24)) atomicAdd(&l.count[(key >> sh) & 255], 1u);
+      __syncthreads();
+      if (wave == 0) {                                   // four bins a lane, the largest first
+        uint32_t c[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += c[i] = l.count[255 - 4 * lane - i];
+        uint32_t before = wave_scan(sum, lane) - sum;
+        if (lane == 63) l.found[0] = before + sum < left ? ~0ull : 0;      // fewer maxima than k: every token is taken
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (before < left && before + c[i] >= left) { l.found[1] = 255 - 4 * lane - i; l.found[2] = before; }
+          before += c[i];
+        }
       }
       __syncthreads();
-      if (nk <= kSampleCount) {
-        for_pairs(nk, tid, [&](int i, int from, int to) {
-          const uint32_t x = (uint32_t)s_list[i];        // the complement of the index
-          uint64_t sum = 0;
-          for (int j = from; j < to; ++j) sum += (uint32_t)s_list[j] > x ? s_mass[j] : 0;
-          if (sum) atomicAdd((unsigned long long*)&s_mass[kSampleShortK + i], (unsigned long long)sum);
-        });
-        __syncthreads();
-        const uint64_t before = tid < nk ? s_mass[kSampleShortK + tid] : 0;
-        if (kept && before <= want && before + w > want) answer((int64_t)(uint32_t)~(uint32_t)place, (float)((double)w / (double)all));
-        return;
-      }
-      sort_falling(s_list, kSampleShortK, tid);
-      const uint64_t entry = tid < kSampleShortK ? s_list[tid] : 0;
-      // (an entry of 0 would be index 2^32 - 1, which no row has)
-      const uint64_t wi = entry ? s_mass[(uint32_t)entry] : 0;
-      const uint64_t by_index = block_scan(wi, s_sum, wave, lane, all);
-      if (wi && by_index > want && by_index - wi <= want) answer((int64_t)(uint32_t)~(uint32_t)(entry >> 32), (float)((double)wi / (double)all));
-      return;
+      if (l.found[0]) { prefix = 0; break; }
+      prefix |= (uint32_t)l.found[1] << sh;
+      left -= (uint32_t)l.found[2];
+      __syncthreads();
+    }
+    collect(of_key(max(prefix, kKeyNone + 1)), [](float f) { return f > -__builtin_inff(); });
+    const int n = l.n;
+    __syncthreads();
+    if (n > kSampleList) return false;
+    order_list(n);
+    const int nk = (int)min((int64_t)n, rs.k);           // at most 512: one a thread
+    const uint64_t place = tid < nk ? l.list[tid] : 0, w = tid < nk ? weigh(of_key(place >> 32)) : 0;
+    uint64_t total, all;
+    const uint64_t upto = block_scan(w, l.sum, wave, lane, total);
+    const bool kept = w >= least && (rs.p >= 1.0 || upto - w < share_of(rs.p, total));
+    block_scan(kept ? w : 0, l.sum, wave, lane, all);
+    const uint64_t want = number(all);
+    // what is kept before a token by index: of few by pairs, else along the list sorted by index
+    if (tid < kSampleShortK) {
+      l.mass[tid] = kept ? w : 0;
+      l.mass[kSampleShortK + tid] = 0;
+      if (nk > kSampleCount) l.list[tid] = kept ? place << 32 | (uint32_t)tid : 0;
     }
     __syncthreads();
-    if (tid == 0) s_n = 0;
+    if (nk <= kSampleCount) {
+      for_pairs(nk, tid, [&](int i, int from, int to) {
+        const uint32_t x = (uint32_t)l.list[i];          // the complement of the index
+        uint64_t sum = 0;
+        for (int j = from; j < to; ++j) sum += (uint32_t)l.list[j] > x ? l.mass[j] : 0;
+        if (sum) atomicAdd((unsigned long long*)&l.mass[kSampleShortK + i], (unsigned long long)sum);
+      });
+      __syncthreads();
+      const uint64_t before = tid < nk ? l.mass[kSampleShortK + tid] : 0;
+      if (kept && before <= want && before + w > want) answer((int64_t)(uint32_t)~(uint32_t)place, (float)((double)w / (double)all));
+      return true;
+    }
+    sort_falling(l.list, kSampleShortK, tid);
+    const uint64_t entry = tid < kSampleShortK ? l.list[tid] : 0;
+    // (an entry of 0 would be index 2^32 - 1, which no row has)
+    const uint64_t wi = entry ? l.mass[(uint32_t)entry] : 0;
+    const uint64_t by_index = block_scan(wi, l.sum, wave, lane, all);
+    if (wi && by_index > want && by_index - wi <= want) answer((int64_t)(uint32_t)~(uint32_t)(entry >> 32), (float)((double)wi / (double)all));
+    return true;
   }
 
-  if (rs.k < a.V || rs.p < 1.0) {
-    // ---- weights, and with top-k counts, over bins
-    const bool by_count = rs.k < a.V;
+  // ---- weights (and counts) over bins, of the octets [from, to)
+  __device__ inline void fill_bins(int64_t from, int64_t to, bool by_count) {
     for (int i = tid; i < kSampleBins; i += NT) {
-      s_mass[i] = 0;
-      s_count[i] = 0;
+      l.mass[i] = 0;
+      l.count[i] = 0;
     }
     __syncthreads();
-    for (int64_t o = tid; o < octets; o += NT) {
+    for (int64_t o = from + tid; o < to; o += NT) {
       float f[8];
       load8(o, f);
 #pragma unroll
@@ -342,100 +383,72 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
         int n;
         const uint64_t w = weigh(f[i], n);
         if (w) {
-          atomicAdd((unsigned long long*)&s_mass[weigh.bin(n)], (unsigned long long)w);
-          if (by_count) atomicAdd(&s_count[weigh.bin(n)], 1u);
+          atomicAdd((unsigned long long*)&l.mass[weigh.bin(n)], (unsigned long long)w);
+          if (by_count) atomicAdd(&l.count[weigh.bin(n)], 1u);
         }
       }
     }
     __syncthreads();
-    uint64_t total;
-    const uint64_t m0 = s_mass[2 * tid], m1 = s_mass[2 * tid + 1];
-    uint64_t mass_before = block_scan(m0 + m1, s_sum, wave, lane, total) - m0 - m1;
-    // The place at which a filter ends: the smallest beginning of the order with `want` tokens or weight.  Returns the weight from it on.
-    const auto end_in = [&](bool mass, uint64_t want, uint64_t before, uint64_t c0, uint64_t c1, uint64_t above_mass) {
-      __syncthreads();
-      if (before < want && before + c0 >= want) { s_found[0] = 2 * tid; s_found[1] = before; s_found[2] = above_mass; }
-      if (before + c0 < want && before + c0 + c1 >= want) { s_found[0] = 2 * tid + 1; s_found[1] = before + c0; s_found[2] = above_mass + m0; }
-      if (tid == 0) s_n = 0;
-      __syncthreads();
-      const int bin = (int)s_found[0];
-      uint64_t above = s_found[1], mass_above = s_found[2];
-      __syncthreads();
-      const auto in_bin = [&](float f) { int n; return weigh(f, n) != 0 && weigh.bin(n) == bin; };
-      // (bounds of the bin's logits with room for y's rounding, so that the other octets are passed over)
-      collect((float)((double)M + (-8.0 * bin - 9.0) / weigh.k) - 1e-5f * fabsf(M), in_bin);
-      const int n = s_n;
-      __syncthreads();
-      if (n <= kSampleList) {
-        pad_and_sort(n);
-        // four a thread
-        uint64_t w[4], sum = 0, whole;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += w[i] = 4 * tid + i < n ? weigh(of_key(s_list[4 * tid + i] >> 32)) : 0;
-        uint64_t upto = mass_above + block_scan(sum, s_sum, wave, lane, whole) - sum;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = 4 * tid + i;
-          const bool here = at < n && (mass ? upto < want && upto + w[i] >= want : above + at + 1 == want);
-          upto += w[i];
-          if (here) { s_found[0] = s_list[at]; s_found[1] = upto; }
-        }
-      } else {
-        // too many for the list: a radix search over the bin's places, 8 bits at a time
-        uint64_t prefix = 0;
-        for (int sh = 56; sh >= 0; sh -= 8) {
-          __syncthreads();
-          if (tid < 256) { s_list[tid] = 0; s_list[256 + tid] = 0; }
-          __syncthreads();
-          for (int64_t o = tid; o < octets; o += NT) {
-            float f[8];
-            load8(o, f);
-#pragma unroll 1
-            for (int i = 0; i < 8; ++i) {
-              const uint64_t p = place_of(f[i], o * 8 + i);
-              if (in_bin(f[i]) && (sh == 56 || p >> (sh + 8) == prefix >> (sh + 8))) {
-                atomicAdd((unsigned long long*)&s_list[(p >> sh) & 255], (unsigned long long)weigh(f[i]));
-                atomicAdd((unsigned long long*)&s_list[256 + ((p >> sh) & 255)], 1ull);
-              }
-            }
-          }
-          __syncthreads();
-          if (tid == 0) {
-            int b = 255;
-            for (; b > 0; --b) {
-              if ((mass ? mass_above + s_list[b] : above + s_list[256 + b]) >= want) break;
-              above += s_list[256 + b];
-              mass_above += s_list[b];
-            }
-            s_found[0] = b; s_found[1] = above; s_found[2] = mass_above;
-            if (sh == 0) s_list[0] = mass_above + s_list[b];
-          }
-          __syncthreads();
-          prefix |= s_found[0] << sh;
-          above = s_found[1];
-          mass_above = s_found[2];
-        }
-        if (tid == 0) { s_found[0] = prefix; s_found[1] = s_list[0]; }
-      }
-      __syncthreads();
-      edge = s_found[0];
-      low = of_key(edge >> 32);
-      return s_found[1];
-    };
-    if (by_count) {
-      uint64_t live;
-      const uint64_t n0 = s_count[2 * tid], n1 = s_count[2 * tid + 1];
-      const uint64_t before = block_scan(n0 + n1, s_sum, wave, lane, live) - n0 - n1;
-      if ((uint64_t)rs.k < live) total = end_in(false, (uint64_t)rs.k, before, n0, n1, mass_before);
-    }
-    if (rs.p < 1.0) end_in(true, share_of(rs.p, total), mass_before, m0, m1, mass_before);
   }
 
-  // ---- kept weight by segments of the row, each a wave's: 512 elements, or as many times that as the list has places for
-  __syncthreads();
-  const int64_t rounds = (octets + 63) / 64, per = (rounds + kSampleList - 1) / kSampleList;
-  const int segments = (int)((rounds + per - 1) / per);
-  const auto kept8 = [&](int64_t o, uint64_t (&w)[8]) {  // weights of an octet's kept tokens; their sum
+  // The filter's end, from the bin in found: edge, low.  Returns the weight down to it.
+  __device__ inline uint64_t end_in_bin(bool by_mass, uint64_t want) {
+    const int bin = (int)l.found[0];
+    uint64_t above = l.found[1], mass_above = l.found[2];
+    if (tid == 0) l.n = 0;
+    __syncthreads();
+    const auto in_bin = [&](float f) { int n; return weigh(f, n) != 0 && weigh.bin(n) == bin; };
+    collect(bin_floor(bin), in_bin);
+    const int n = l.n;
+    __syncthreads();
+    if (n <= kSampleList) {
+      cut_list(n, by_mass, want, above, mass_above);
+    } else {
+      // too many for the list: a radix search over the bin's places, 8 bits at a time
+      uint64_t prefix = 0;
+      for (int sh = 56; sh >= 0; sh -= 8) {
+        __syncthreads();
+        if (tid < 256) { l.list[tid] = 0; l.list[256 + tid] = 0; }
+        __syncthreads();
+        for (int64_t o = tid; o < octets; o += NT) {
+          float f[8];
+          load8(o, f);
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            const uint64_t p = place_of(f[i], o * 8 + i);
+            if (in_bin(f[i]) && (sh == 56 || p >> (sh + 8) == prefix >> (sh + 8))) {
+              atomicAdd((unsigned long long*)&l.list[(p >> sh) & 255], (unsigned long long)weigh(f[i]));
+              atomicAdd((unsigned long long*)&l.list[256 + ((p >> sh) & 255)], 1ull);
+            }
+          }
+        }
+        __syncthreads();
+        if (tid == 0) {
+          int b = 255;
+          for (; b > 0; --b) {
+            if ((by_mass ? mass_above + l.list[b] : above + l.list[256 + b]) >= want) break;
+            above += l.list[256 + b];
+            mass_above += l.list[b];
+          }
+          l.found[0] = b; l.found[1] = above; l.found[2] = mass_above;
+          if (sh == 0) l.list[0] = mass_above + l.list[b];
+        }
+        __syncthreads();
+        prefix |= l.found[0] << sh;
+        above = l.found[1];
+        mass_above = l.found[2];
+      }
+      __syncthreads();
+      if (tid == 0) { l.found[0] = prefix; l.found[1] = l.list[0]; }
+      __syncthreads();
+    }
+    edge = l.found[0];
+    low = of_key(edge >> 32);
+    return l.found[1];
+  }
+
+  // Weights of an octet's kept tokens, and their sum.
+  __device__ inline uint64_t kept8(int64_t o, uint64_t (&w)[8]) const {
     uint64_t sum = 0;
     float f[8];
     const bool in = o < octets;
@@ -452,41 +465,201 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
       for (int i = 0; i < 8; ++i) w[i] = 0;
     }
     return sum;
-  };
-  for (int s = wave; s < segments; s += kSampleWaves) {
-    uint64_t sum = 0, w[8];
-    for (int64_t i = 0; i < per; ++i) sum += kept8((s * per + i) * 64 + lane, w);
-    sum = wave_reduce(sum, [](uint64_t p, uint64_t q) { return p + q; });
-    if (lane == 0) s_list[s] = sum;
   }
-  __syncthreads();
-  uint64_t w4[4], sum = 0, all;
+  // ---- the token, from the segments' kept weight in list
+  __device__ inline void draw() {
+    uint64_t w4[4], sum = 0, all;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) sum += w4[i] = 4 * tid + i < segments ? s_list[4 * tid + i] : 0;
-  uint64_t before = block_scan(sum, s_sum, wave, lane, all) - sum;
-  uint64_t want = (uint64_t)(rs.u * (double)all);
-  if (want >= all) want = all - 1;
+    for (int i = 0; i < 4; ++i) sum += w4[i] = 4 * tid + i < segments ? l.list[4 * tid + i] : 0;
+    uint64_t before = block_scan(sum, l.sum, wave, lane, all) - sum;
+    const uint64_t want = number(all);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (before <= want && before + w4[i] > want) { s_found[0] = 4 * tid + i; s_found[1] = before; }
-    before += w4[i];
-  }
-  __syncthreads();
-  if (wave != 0) return;
-  // ---- and the token inside its segment
-  before = s_found[1];
-  for (int64_t i = 0; i < per; ++i) {
-    const int64_t o = ((int64_t)s_found[0] * per + i) * 64 + lane;
-    uint64_t w[8];
-    const uint64_t mine8 = kept8(o, w), upto = wave_scan(mine8, lane);
-    uint64_t at = before + upto - mine8;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (at <= want && at + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
-      at += w[j];
+    for (int i = 0; i < 4; ++i) {
+      if (before <= want && before + w4[i] > want) { l.found[0] = 4 * tid + i; l.found[1] = before; }
+      before += w4[i];
     }
-    before += __shfl(upto, 63);
+    __syncthreads();
+    if (wave != 0) return;
+    before = l.found[1];
+    for (int64_t i = 0; i < per; ++i) {
+      const int64_t o = ((int64_t)l.found[0] * per + i) * 64 + lane;
+      uint64_t w[8];
+      const uint64_t mine = kept8(o, w), upto = wave_scan(mine, lane);
+      uint64_t at = before + upto - mine;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (at <= want && at + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
+        at += w[j];
+      }
+      before += __shfl(upto, 63);
+    }
   }
+
+  // ---- a row by one workgroup
+  __device__ inline void whole() {
+    float mine = largest(0, octets), M = wave_max(mine);
+    if (lane == 0) l.max[wave] = M;
+    __syncthreads();
+    M = slots_reduce<kSampleWaves>(l.max, lane, [](float p, float q) { return fmaxf(p, q); });
+    if (M == -__builtin_inff()) {
+      if (tid == 0) answer(-1, 0.0f);
+      return;
+    }
+    set_max(M);
+    if (infinite) mine = mine == __builtin_inff() ? 0.0f : -__builtin_inff();
+    if (rs.k <= kSampleShortK && short_list(mine)) return;
+    if (rs.k < a.V || rs.p < 1.0) {
+      __syncthreads();
+      fill_bins(0, octets, rs.k < a.V);
+      uint64_t total;
+      const uint64_t m0 = l.mass[2 * tid], m1 = l.mass[2 * tid + 1], n0 = l.count[2 * tid], n1 = l.count[2 * tid + 1];
+      const uint64_t mass_before = block_scan(m0 + m1, l.sum, wave, lane, total) - m0 - m1;
+      if (rs.k < a.V) {
+        uint64_t live;
+        const uint64_t before = block_scan(n0 + n1, l.sum, wave, lane, live) - n0 - n1;
+        if ((uint64_t)rs.k < live) {
+          find_bin((uint64_t)rs.k, before, n0, n1, mass_before, m0);
+          total = end_in_bin(false, (uint64_t)rs.k);
+        }
+      }
+      if (rs.p < 1.0) {
+        const uint64_t want = share_of(rs.p, total);
+        find_bin(want, mass_before, m0, m1, mass_before, m0);
+        end_in_bin(true, want);
+      }
+    }
+    __syncthreads();
+    for (int s = wave; s < segments; s += kSampleWaves) {
+      uint64_t sum = 0, w[8];
+      for (int64_t i = 0; i < per; ++i) sum += kept8((s * per + i) * 64 + lane, w);
+      sum = wave_reduce(sum, [](uint64_t p, uint64_t q) { return p + q; });
+      if (lane == 0) l.list[s] = sum;
+    }
+    __syncthreads();
+    draw();
+  }
+
+  // ---- a row by several: this workgroup's segments [s0, s1)
+  __device__ inline SampleWs* shared_state() const { return (SampleWs*)(a.ws + row * kSampleRowBytes); }
+  __device__ inline void my_segments(int& s0, int& s1) const {
+    const int each = (segments + a.parts - 1) / a.parts, part = (int)(blockIdx.x % a.parts);
+    s0 = min(segments, part * each);
+    s1 = min(segments, s0 + each);
+  }
+  // The row's largest logit from its parts'; false where there is nothing for the split form to do.
+  __device__ inline bool split_max() {
+    const float M = wave_max(lane < a.parts ? shared_state()->max[lane] : -__builtin_inff());
+    if (M == -__builtin_inff() || rs.k < a.V) return false;       // (a greedy row has k = 1: the last launch takes it whole)
+    set_max(M);
+    return true;
+  }
+  __device__ inline void part_max() {
+    SampleWs* ws = shared_state();
+    const int part = (int)(blockIdx.x % a.parts);
+    int s0, s1;
+    my_segments(s0, s1);
+    const float M = wave_max(largest(s0 * per * 64, min(octets, s1 * per * 64)));
+    if (lane == 0) l.max[wave] = M;
+    for (int i = part * NT + tid; i < kSampleBins; i += a.parts * NT) ws->mass[i] = 0;
+    __syncthreads();
+    if (wave == 0) {
+      const float top = slots_reduce<kSampleWaves>(l.max, lane, [](float p, float q) { return fmaxf(p, q); });
+      if (lane == 0) ws->max[part] = top;
+      if (lane == 0 && part == 0) ws->n = 0;
+    }
+  }
+  __device__ inline void part_bins() {
+    if (rs.p >= 1.0 || !split_max()) return;
+    int s0, s1;
+    my_segments(s0, s1);
+    fill_bins(s0 * per * 64, min(octets, s1 * per * 64), false);
+    for (int i = tid; i < kSampleBins; i += NT)
+      if (l.mass[i]) atomicAdd((unsigned long long*)&shared_state()->mass[i], (unsigned long long)l.mass[i]);
+  }
+  // Into found: the bin in which top-p ends.  Returns the weight that it asks for.
+  __device__ inline uint64_t split_bin() {
+    const SampleWs* ws = shared_state();
+    uint64_t total;
+    const uint64_t m0 = ws->mass[2 * tid], m1 = ws->mass[2 * tid + 1];
+    const uint64_t mass_before = block_scan(m0 + m1, l.sum, wave, lane, total) - m0 - m1, want = share_of(rs.p, total);
+    find_bin(want, mass_before, m0, m1, mass_before, m0);
+    return want;
+  }
+  __device__ inline void part_sums() {
+    if (!split_max()) return;
+    SampleWs* ws = shared_state();
+    int bin = kSampleBins, s0, s1;
+    if (rs.p < 1.0) {
+      split_bin();
+      bin = (int)l.found[0];
+      low = bin_floor(bin);
+    }
+    my_segments(s0, s1);
+    for (int s = s0 + wave; s < s1; s += kSampleWaves) {
+      uint64_t sum = 0;
+      for (int64_t i = 0; i < per; ++i) {
+        const int64_t o = (s * per + i) * 64 + lane;
+        float f[8];
+        if (o < octets) load8(o, f);
+        if (o < octets && max8(f) >= low) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            int n;
+            const uint64_t w = weigh(f[j], n);
+            const int b = weigh.bin(n);
+            if (b < bin && w >= least) sum += w;
+            if (b == bin && w) {
+              const uint32_t at = atomicAdd(&ws->n, 1u);
+              if (at < (uint32_t)kSampleList) ws->list[at] = place_of(f[j], o * 8 + j);
+            }
+          }
+        }
+      }
+      sum = wave_reduce(sum, [](uint64_t p, uint64_t q) { return p + q; });
+      if (lane == 0) ws->segment[s] = sum;
+    }
+  }
+  __device__ inline void split_draw() {
+    const SampleWs* ws = shared_state();
+    const int n = (int)min(ws->n, (uint32_t)kSampleList + 1);
+    if (n > kSampleList || !split_max()) return whole();
+    if (rs.p < 1.0) {
+      const uint64_t want = split_bin(), above = l.found[1], mass_above = l.found[2];
+      for (int i = tid; i < n; i += NT) l.list[i] = ws->list[i];
+      __syncthreads();
+      cut_list(n, true, want, above, mass_above);
+      edge = l.found[0];
+      low = of_key(edge >> 32);
+      uint64_t place[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) place[i] = i * NT + tid < n ? l.list[i * NT + tid] : 0;
+      __syncthreads();
+      for (int i = tid; i < segments; i += NT) l.list[i] = ws->segment[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (place[i] >= edge) {                          // (no place is 0)
+          const uint64_t w = weigh(of_key(place[i] >> 32));
+          if (w >= least) atomicAdd((unsigned long long*)&l.list[(uint32_t)~(uint32_t)place[i] / (uint32_t)(per * 512)], (unsigned long long)w);
+        }
+    } else {
+      for (int i = tid; i < segments; i += NT) l.list[i] = ws->segment[i];
+    }
+    __syncthreads();
+    draw();
+  }
+};
+
+enum : int { SAMPLE_WHOLE = 0, SAMPLE_MAX = 1, SAMPLE_BINS = 2, SAMPLE_SUMS = 3, SAMPLE_DRAW = 4 };
+template <class T, int STEP>
+__global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
+  __shared__ SampleLds lds;
+  Sampler<T> s(a, lds, STEP == SAMPLE_WHOLE || STEP == SAMPLE_DRAW ? blockIdx.x : blockIdx.x / a.parts);
+  if constexpr (STEP == SAMPLE_WHOLE) s.whole();
+  else if constexpr (STEP == SAMPLE_MAX) s.part_max();
+  else if constexpr (STEP == SAMPLE_BINS) s.part_bins();
+  else if constexpr (STEP == SAMPLE_SUMS) s.part_sums();
+  else s.split_draw();
 }
 
 }  // namespace elmo
