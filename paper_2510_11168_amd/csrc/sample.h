@@ -183,8 +183,9 @@ template <class T> struct Sampler {
   const RowSettings rs;
   bool infinite = false;                       // the largest logit is +infinity: only such have a weight; 0 stands for it, -infinity for the others
   Weigh weigh;
-  uint64_t least = 1, edge = (uint64_t)(kKeyNone + 1) << 32;     // smallest kept weight; kept: places from here on
-  float low = -__builtin_inff();                                 // no kept logit lies below this
+  uint64_t least = 1;                                            // smallest kept weight
+  float low = -__builtin_inff();                                 // smallest kept logit,
+  uint32_t last = ~0u;                                           // and of those equal to it the last kept index
 
   __device__ inline Sampler(const SampleArgs& args, SampleLds& lds, int64_t r)
       : a(args), l(lds), row(r), octets((args.V + 7) >> 3), per(((octets + 63) / 64 + kSampleList - 1) / kSampleList),
@@ -378,20 +379,25 @@ template <class T> struct Sampler {
     for (int64_t o = from + tid; o < to; o += NT) {
       float f[8];
       load8(o, f);
+      uint64_t w[8];
+      int n[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        int n;
-        const uint64_t w = weigh(f[i], n);
-        if (w) {
-          atomicAdd((unsigned long long*)&l.mass[weigh.bin(n)], (unsigned long long)w);
-          if (by_count) atomicAdd(&l.count[weigh.bin(n)], 1u);
+      for (int i = 0; i < 8; ++i) w[i] = weigh(f[i], n[i]);      // (all of them before the first branch: eight chains side by side)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (w[i]) {
+          atomicAdd((unsigned long long*)&l.mass[weigh.bin(n[i])], (unsigned long long)w[i]);
+          if (by_count) atomicAdd(&l.count[weigh.bin(n[i])], 1u);
         }
-      }
     }
     __syncthreads();
   }
 
-  // The filter's end, from the bin in found: edge, low.  Returns the weight down to it.
+  __device__ inline void set_edge(uint64_t place) {
+    low = of_key(place >> 32);
+    last = ~(uint32_t)place;
+  }
+  // The filter's end, from the bin in found.  Returns the weight down to it.
   __device__ inline uint64_t end_in_bin(bool by_mass, uint64_t want) {
     const int bin = (int)l.found[0];
     uint64_t above = l.found[1], mass_above = l.found[2];
@@ -442,8 +448,7 @@ template <class T> struct Sampler {
       if (tid == 0) { l.found[0] = prefix; l.found[1] = l.list[0]; }
       __syncthreads();
     }
-    edge = l.found[0];
-    low = of_key(edge >> 32);
+    set_edge(l.found[0]);
     return l.found[1];
   }
 
@@ -454,10 +459,12 @@ template <class T> struct Sampler {
     const bool in = o < octets;
     if (in) load8(o, f);
     if (in && max8(f) >= low) {
+      const uint32_t at = (uint32_t)o * 8;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         w[i] = weigh(f[i]);
-        if (w[i] < least || place_of(f[i], o * 8 + i) < edge) w[i] = 0;
+        const bool kept = f[i] > low || (f[i] == low && at + i <= last);
+        w[i] = kept && w[i] >= least ? w[i] : 0;
         sum += w[i];
       }
     } else {
@@ -602,17 +609,20 @@ template <class T> struct Sampler {
         float f[8];
         if (o < octets) load8(o, f);
         if (o < octets && max8(f) >= low) {
+          uint64_t w[8];
+          int n[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            int n;
-            const uint64_t w = weigh(f[j], n);
-            const int b = weigh.bin(n);
-            if (b < bin && w >= least) sum += w;
-            if (b == bin && w) {
+            w[j] = weigh(f[j], n[j]);
+            n[j] = weigh.bin(n[j]);
+            sum += n[j] < bin && w[j] >= least ? w[j] : 0;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (n[j] == bin && w[j]) {
               const uint32_t at = atomicAdd(&ws->n, 1u);
               if (at < (uint32_t)kSampleList) ws->list[at] = place_of(f[j], o * 8 + j);
             }
-          }
         }
       }
       sum = wave_reduce(sum, [](uint64_t p, uint64_t q) { return p + q; });
@@ -628,8 +638,8 @@ template <class T> struct Sampler {
       for (int i = tid; i < n; i += NT) l.list[i] = ws->list[i];
       __syncthreads();
       cut_list(n, true, want, above, mass_above);
-      edge = l.found[0];
-      low = of_key(edge >> 32);
+      const uint64_t edge = l.found[0];
+      set_edge(edge);
       uint64_t place[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) place[i] = i * NT + tid < n ? l.list[i * NT + tid] : 0;
