@@ -237,32 +237,39 @@ constexpr int64_t kMostV = ((int64_t)1 << 31) - 1;
 }
 
 namespace {
-// Workgroups of a row without top-k: one where the rows fill the chip or are short.
-int sample_parts(int64_t rows, int64_t V) {
-  if (rows > 128 || V < 16384) return 1;
+// Workgroups of a row without top-k: one where the rows fill the chip or are short.  Rows of 131072, top-p: 128 in FP32 67 us split (121 whole), in BF16,
+// which one workgroup takes by codes, 68 split and 58 whole; 1 row 28 and 120.  One row of 8192 FP32: 25.6 split, 18.9 whole.
+constexpr int64_t kSampleSplitRows = 128, kSampleSplitV = 16384;
+int sample_parts(int64_t rows, int64_t V, bool bf16) {
+  if (rows > (bf16 ? kSampleSplitRows / 2 : kSampleSplitRows) || V < kSampleSplitV) return 1;
   return (int)std::min<int64_t>(std::min<int64_t>(64, (V + 4095) / 4096), std::max<int64_t>(2, 256 / rows));
+}
+template <class T, int STEP> int launch_sample_step(const elmo::SampleArgs& a, unsigned grid, hipStream_t st) {
+  constexpr int smem = elmo::sample_smem<T, STEP>();
+  static_assert(smem + sizeof(elmo::SampleLds) <= 160 * 1024, "LDS of a row");
+  if constexpr (smem > 0) {
+    static std::once_flag once;
+    static hipError_t attr_rc = hipSuccess;
+    std::call_once(once, [] {
+      attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&elmo::k_sample<T, STEP>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    });
+    if (attr_rc != hipSuccess) return fail(-3, "hipFuncSetAttribute(k_sample) failed: %s", hipGetErrorString(attr_rc));
+  }
+  elmo::k_sample<T, STEP><<<grid, elmo::kSampleThreads, smem, st>>>(a);
+  return check_launch("k_sample");
 }
 template <class T> int launch_sample(const elmo::SampleArgs& a, int64_t rows, hipStream_t st) {
   const unsigned one = (unsigned)rows, all = (unsigned)(rows * a.parts);
-  if (a.parts == 1) {
-    elmo::k_sample<T, elmo::SAMPLE_WHOLE><<<one, elmo::kSampleThreads, 0, st>>>(a);
-    return check_launch("k_sample");
-  }
-  elmo::k_sample<T, elmo::SAMPLE_MAX><<<all, elmo::kSampleThreads, 0, st>>>(a);
-  ELMO_TRY(check_launch("k_sample (maxima)"));
-  if (a.top_p) {
-    elmo::k_sample<T, elmo::SAMPLE_BINS><<<all, elmo::kSampleThreads, 0, st>>>(a);
-    ELMO_TRY(check_launch("k_sample (bins)"));
-  }
-  elmo::k_sample<T, elmo::SAMPLE_SUMS><<<all, elmo::kSampleThreads, 0, st>>>(a);
-  ELMO_TRY(check_launch("k_sample (sums)"));
-  elmo::k_sample<T, elmo::SAMPLE_DRAW><<<one, elmo::kSampleThreads, 0, st>>>(a);
-  return check_launch("k_sample (draw)");
+  if (a.parts == 1) return launch_sample_step<T, elmo::SAMPLE_WHOLE>(a, one, st);
+  ELMO_TRY((launch_sample_step<T, elmo::SAMPLE_MAX>(a, all, st)));
+  if (a.top_p) ELMO_TRY((launch_sample_step<T, elmo::SAMPLE_BINS>(a, all, st)));
+  ELMO_TRY((launch_sample_step<T, elmo::SAMPLE_SUMS>(a, all, st)));
+  return launch_sample_step<T, elmo::SAMPLE_DRAW>(a, one, st);
 }
 }  // namespace
 
 extern "C" size_t elmo_sample_bytes(int64_t rows, int64_t V) {
-  return rows < 1 || V < 1 || sample_parts(rows, V) == 1 ? 0 : (size_t)rows * elmo::kSampleRowBytes;
+  return rows < 1 || rows > kSampleSplitRows || V < kSampleSplitV ? 0 : (size_t)rows * elmo::kSampleRowBytes;
 }
 
 extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const float* u, const float* temperature,
@@ -283,7 +290,7 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return fail(-1, "workspace missing, smaller than %zu bytes or not 256-byte aligned", need);
   // (with top-k the few tokens that stay are found faster by one workgroup)
   const elmo::SampleArgs a{logits, logits_stride, V, u, temperature, top_p, min_p, top_k, idx_out, prob_out, std::min(50, 62 - bits),
-                           top_k ? 1 : sample_parts(rows, V), (char*)workspace};
+                           top_k ? 1 : sample_parts(rows, V, dtype == ELMO_BF16), (char*)workspace};
   hipStream_t st = (hipStream_t)hip_stream;
   return dtype == ELMO_BF16 ? launch_sample<uint16_t>(a, rows, st) : launch_sample<float>(a, rows, st);
 }

@@ -13,6 +13,8 @@
 //                  which is sorted, filtered and drawn from: two readings, no weights but the list's;
 //   top_p, top_k   counts and weights over bins of 1/32 octave of weight, then the tokens of the bin in which the filter ends, sorted (a bin
 //                  that holds too many: a radix search over their places); three readings, four with both;
+//   BF16           in place of the bins, counts of the logits' codes: a weight is computed once a code, and the place at which a filter ends
+//                  is a code and a number of tokens that have it;
 //   otherwise      sums of the kept weights over segments of the row, and the token inside the segment on which the number falls.
 // Few long rows without top-k go over several workgroups each, in four launches: maxima; bins; sums of the segments without the bin in which top-p ends,
 // whose tokens go to a list; and by one workgroup the list, its kept tokens added to their segments, and the draw.
@@ -171,6 +173,14 @@ struct SampleWs {
   uint32_t n;
 };
 constexpr size_t kSampleRowBytes = (sizeof(SampleWs) + 255) / 256 * 256;
+
+// A BF16 row has few logits that carry weight: the codes of both signs over 21 octaves below the larger end of [smallest logit with a weight, largest
+// logit].  Slots in falling order.  (Logits nearer to zero than that, should there be any, send a row the other way.)
+constexpr int kCodeOctaves = 21, kCodeHalf = kCodeOctaves * 128, kCodes = 2 * kCodeHalf, kCodesEach = (kCodes + kSampleThreads - 1) / kSampleThreads;
+struct SampleCodes {
+  uint64_t weight[kCodesEach * kSampleThreads];
+  uint32_t count[kCodesEach * kSampleThreads];
+};
 
 // One row in the hands of a workgroup.
 template <class T> struct Sampler {
@@ -502,8 +512,210 @@ template <class T> struct Sampler {
     }
   }
 
+  // ---- BF16, by codes.  False: not this row.
+  __device__ inline int slot(uint32_t code, int base) const {    // negative or beyond kCodes: none
+    const int i = (int)(code & 0x7FFF) - base;
+    const int s = code & 0x8000 ? kCodeHalf + i : kCodeHalf - 1 - i;
+    return (uint32_t)i < (uint32_t)kCodeHalf ? s : -1;
+  }
+  __device__ inline bool by_code(SampleCodes* c) {
+    if (infinite) return false;
+    const float bottom = (float)(weigh.M + weigh.least / weigh.k);       // (-infinity at a temperature of infinity)
+    const uint32_t wide = f2u(fmaxf(fabsf((float)weigh.M), fminf(fabsf(bottom), 3.3e38f))) >> 23;   // exponents up to this one
+    const int base = max(0, (int)wide - (kCodeOctaves - 1)) * 128;
+    if (base == 0) return false;                                         // (both zeros would have codes)
+    const int s0 = kCodesEach * tid;
+#pragma unroll
+    for (int i = 0; i < kCodesEach; ++i) {
+      const int s = s0 + i;
+      const uint32_t code = s < kCodeHalf ? base + kCodeHalf - 1 - s : 0x8000u + base + s - kCodeHalf;
+      const float f = u2f(code << 16);
+      c->weight[s] = s < kCodes && f <= (float)weigh.M ? weigh(f) : 0;
+      c->count[s] = 0;
+    }
+    __syncthreads();
+    int end = kCodes;                                    // slots before this one are kept, of its own tokens the first `ties`
+    uint64_t ties = 0;
+    if (rs.k < a.V || rs.p < 1.0) {
+      uint64_t zero_mass = 0, zero_tokens = 0;           // of the logits nearer to zero
+#pragma unroll 4
+      for (int64_t o = tid; o < octets; o += NT) {
+        const Octet<uint16_t> oc = load_octet((const uint16_t*)z + o * 8, a.V - o * 8, 0xFF80u);
+        bool small = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t code = (i & 1) ? oc.v[i >> 1] >> 16 : oc.v[i >> 1] & 0xFFFFu;
+          const int s = slot(code, base);
+          small |= (int)(code & 0x7FFF) < base;
+          if (s >= 0) atomicAdd(&c->count[s], 1u);
+        }
+        if (small) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if ((int)(f2u(oc[i]) >> 16 & 0x7FFF) < base) {
+              const uint64_t w = weigh(oc[i]);
+              zero_mass += w;
+              zero_tokens += w != 0;
+            }
+        }
+      }
+      block_scan(zero_mass, l.sum, wave, lane, zero_mass);
+      block_scan(zero_tokens, l.sum, wave, lane, zero_tokens);
+      __syncthreads();
+      // a thread's six slots
+      uint64_t w[kCodesEach], n[kCodesEach], mass = 0, tokens = 0, total, live;
+#pragma unroll
+      for (int i = 0; i < kCodesEach; ++i) {
+        w[i] = c->weight[s0 + i];
+        n[i] = w[i] ? c->count[s0 + i] : 0;
+        mass += w[i] * n[i];
+        tokens += n[i];
+      }
+      static_assert(kCodeHalf % kCodesEach == 0, "a thread has slots of one sign");
+      const bool negative = s0 >= kCodeHalf;             // behind the logits next to zero
+      const uint64_t mass_before = block_scan(mass, l.sum, wave, lane, total) - mass + (negative ? zero_mass : 0);
+      const uint64_t before = block_scan(tokens, l.sum, wave, lane, live) - tokens + (negative ? zero_tokens : 0);
+      total += zero_mass;
+      live += zero_tokens;
+      const auto find = [&](bool by_mass, uint64_t want) {
+        uint64_t at_n = before, at_m = mass_before;
+        __syncthreads();
+        if (tid == 0) l.found[0] = kCodes;               // (stays so if the filter ends next to zero)
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kCodesEach; ++i) {
+          const uint64_t at = by_mass ? at_m : at_n, step = by_mass ? w[i] * n[i] : n[i];
+          if (at < want && at + step >= want) {
+            const uint64_t some = by_mass ? (want - at + w[i] - 1) / w[i] : want - at;
+            l.found[0] = s0 + i;
+            l.found[1] = some;
+            l.found[2] = at_m + some * w[i];
+          }
+          at_n += n[i];
+          at_m += w[i] * n[i];
+        }
+        __syncthreads();
+        end = (int)l.found[0];
+        ties = l.found[1];
+        return l.found[2];
+      };
+      if ((uint64_t)rs.k < live) {
+        total = find(false, (uint64_t)rs.k);
+        if (end == kCodes) return false;
+      }
+      if (rs.p < 1.0) {
+        find(true, share_of(rs.p, total));
+        if (end == kCodes) return false;
+      }
+    }
+    const bool keep_zero = end >= kCodeHalf;
+    // what is not kept has no weight from here on; the last code's tokens count apart
+    uint64_t we = end < kCodes ? c->weight[end] : 0;
+    if (we < least) we = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kCodesEach; ++i)
+      if (s0 + i >= end || c->weight[s0 + i] < least) c->weight[s0 + i] = 0;
+    __syncthreads();
+    // an octet's weights without the last code's, and which of it are that
+    const auto octet = [&](int64_t o, uint64_t (&w)[8], uint32_t& mask) {
+      uint64_t sum = 0;
+      mask = 0;
+      bool small = false;
+      if (o < octets) {
+        const Octet<uint16_t> oc = load_octet((const uint16_t*)z + o * 8, a.V - o * 8, 0xFF80u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t code = (i & 1) ? oc.v[i >> 1] >> 16 : oc.v[i >> 1] & 0xFFFFu;
+          const int s = slot(code, base);
+          small |= (int)(code & 0x7FFF) < base;
+          w[i] = s >= 0 ? c->weight[s] : 0;
+          mask |= s == end ? 1u << i : 0;
+          sum += w[i];
+        }
+        if (small && keep_zero) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if ((int)(f2u(oc[i]) >> 16 & 0x7FFF) < base) {
+              w[i] = weigh(oc[i]);
+              if (w[i] < least) w[i] = 0;
+              sum += w[i];
+            }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 0;
+      }
+      return sum;
+    };
+    for (int s = wave; s < segments; s += kSampleWaves) {
+      uint64_t sum = 0, w[8];
+      uint32_t count = 0, mask;
+      for (int64_t i = 0; i < per; ++i) {
+        sum += octet((s * per + i) * 64 + lane, w, mask);
+        count += __popc(mask);
+      }
+      sum = wave_reduce(sum, [](uint64_t p, uint64_t q) { return p + q; });
+      count = wave_reduce(count, [](uint32_t p, uint32_t q) { return p + q; });
+      if (lane == 0) {
+        l.list[s] = sum;
+        c->count[s] = count;
+      }
+    }
+    __syncthreads();
+    // the segments' last-code tokens that are kept are the first `ties` of all of them
+    uint32_t n4[4], some = 0, whole_count;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) some += n4[i] = 4 * tid + i < segments ? c->count[4 * tid + i] : 0;
+    uint32_t seen = block_scan(some, l.sum32, wave, lane, whole_count) - some;
+    uint64_t w4[4], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t left = ties > seen ? ties - seen : 0;
+      w4[i] = 4 * tid + i < segments ? l.list[4 * tid + i] + min((uint64_t)n4[i], left) * we : 0;
+      sum += w4[i];
+      seen += n4[i];
+    }
+    seen -= some;
+    uint64_t at = block_scan(sum, l.sum, wave, lane, all) - sum;
+    const uint64_t want = number(all);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (at <= want && at + w4[i] > want) { l.found[0] = 4 * tid + i; l.found[1] = at; l.found[2] = seen; }
+      at += w4[i];
+      seen += n4[i];
+    }
+    __syncthreads();
+    if (wave != 0) return true;
+    at = l.found[1];
+    uint64_t ranked = l.found[2];
+    for (int64_t i = 0; i < per; ++i) {
+      const int64_t o = ((int64_t)l.found[0] * per + i) * 64 + lane;
+      uint64_t w[8], mine = 0;
+      uint32_t mask;
+      octet(o, w, mask);
+      const uint32_t own = __popc(mask), upto_n = wave_scan(own, lane);
+      uint64_t rank = ranked + upto_n - own;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (mask >> j & 1) w[j] = rank++ < ties ? we : 0;
+        mine += w[j];
+      }
+      const uint64_t upto = wave_scan(mine, lane);
+      uint64_t here = at + upto - mine;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (here <= want && here + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
+        here += w[j];
+      }
+      at += __shfl(upto, 63);
+      ranked += __shfl(upto_n, 63);
+    }
+    return true;
+  }
+
   // ---- a row by one workgroup
-  __device__ inline void whole() {
+  __device__ inline void whole(SampleCodes* codes) {
     float mine = largest(0, octets), M = wave_max(mine);
     if (lane == 0) l.max[wave] = M;
     __syncthreads();
@@ -515,6 +727,10 @@ template <class T> struct Sampler {
     set_max(M);
     if (infinite) mine = mine == __builtin_inff() ? 0.0f : -__builtin_inff();
     if (rs.k <= kSampleShortK && short_list(mine)) return;
+    if constexpr (sizeof(T) == 2) {
+      __syncthreads();
+      if (by_code(codes)) return;
+    }
     if (rs.k < a.V || rs.p < 1.0) {
       __syncthreads();
       fill_bins(0, octets, rs.k < a.V);
@@ -629,10 +845,10 @@ template <class T> struct Sampler {
       if (lane == 0) ws->segment[s] = sum;
     }
   }
-  __device__ inline void split_draw() {
+  __device__ inline void split_draw(SampleCodes* codes) {
     const SampleWs* ws = shared_state();
     const int n = (int)min(ws->n, (uint32_t)kSampleList + 1);
-    if (n > kSampleList || !split_max()) return whole();
+    if (n > kSampleList || !split_max()) return whole(codes);
     if (rs.p < 1.0) {
       const uint64_t want = split_bin(), above = l.found[1], mass_above = l.found[2];
       for (int i = tid; i < n; i += NT) l.list[i] = ws->list[i];
@@ -661,15 +877,19 @@ template <class T> struct Sampler {
 };
 
 enum : int { SAMPLE_WHOLE = 0, SAMPLE_MAX = 1, SAMPLE_BINS = 2, SAMPLE_SUMS = 3, SAMPLE_DRAW = 4 };
+// Dynamic LDS of a launch: the codes, where a row may be taken whole.
+template <class T, int STEP> constexpr int sample_smem() { return sizeof(T) == 2 && (STEP == SAMPLE_WHOLE || STEP == SAMPLE_DRAW) ? (int)sizeof(SampleCodes) : 0; }
 template <class T, int STEP>
 __global__ __launch_bounds__(kSampleThreads) void k_sample(SampleArgs a) {
   __shared__ SampleLds lds;
+  extern __shared__ __align__(16) char dynamic[];
+  SampleCodes* codes = reinterpret_cast<SampleCodes*>(dynamic);
   Sampler<T> s(a, lds, STEP == SAMPLE_WHOLE || STEP == SAMPLE_DRAW ? blockIdx.x : blockIdx.x / a.parts);
-  if constexpr (STEP == SAMPLE_WHOLE) s.whole();
+  if constexpr (STEP == SAMPLE_WHOLE) s.whole(codes);
   else if constexpr (STEP == SAMPLE_MAX) s.part_max();
   else if constexpr (STEP == SAMPLE_BINS) s.part_bins();
   else if constexpr (STEP == SAMPLE_SUMS) s.part_sums();
-  else s.split_draw();
+  else s.split_draw(codes);
 }
 
 }  // namespace elmo

@@ -304,6 +304,52 @@ def test_sample_rows_of_few_values(b, V, dtype):
         check_tokens(z, u, token.cpu(), prob.cpu(), **s)
 
 
+@pytest.mark.parametrize("rows,V", [(130, 20011), (3, 16384), (129, 16391)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sample_without_top_k_in_one_workgroup_and_in_several(b, rows, V, dtype):
+    """Rows on both sides of the number from which a row is no longer split; among them empty ones, ones of infinities, of zeros, of one
+    value, of values next to zero, far from zero and spread over the whole type."""
+    g = gen(V)
+    z = (2.5 * torch.randn((rows, V), generator=g)).to(dtype)
+    z[0, V // 2:] = -float("inf")
+    z[1, 7], z[1, V - 1] = float("inf"), float("inf")
+    z[2] = torch.where(torch.rand(V, generator=g) < 0.3, 0.0, z[2].float()).to(dtype)
+    if rows > 8:
+        z[3] = -float("inf")
+        z[4] = -3.0
+        z[5] = (1e-6 * torch.randn(V, generator=g)).to(dtype)
+        z[6] = (1000 + 8 * torch.randn(V, generator=g)).to(dtype)
+        z[7] = (1e37 * torch.randn(V, generator=g)).to(dtype)
+        z[8] = -z[2].abs()
+    for kw in (dict(), dict(top_p=0.9), dict(top_p=0.3, t=0.7), dict(min_p=0.05), dict(top_p=0.97, min_p=0.01, t=1.5), dict(t=0.0), dict(top_p=0.5, t=1e30),
+               dict(top_p=0.8, t=1e-3)):
+        u = torch.rand(rows, generator=g)
+        s = {name: torch.full((rows,), v) for name, v in kw.items()}
+        token, prob = torch.full((rows,), -7, dtype=torch.int32, device=DEV), torch.full((rows,), -7.0, device=DEV)
+        on = {("temperature" if name == "t" else name): v.to(DEV) for name, v in s.items()}
+        b.elmo_sample(rows_of(z.to(DEV), 3, 1), u.to(DEV), token, prob_out=prob, **on)
+        check_tokens(z, u, token.cpu(), prob.cpu(), **s)
+        if "t" not in kw:                                    # the same by one workgroup a row: top-k that keeps everything
+            again, prob2 = torch.empty_like(token), torch.empty_like(prob)
+            b.elmo_sample(z.to(DEV), u.to(DEV), again, prob_out=prob2, top_k=torch.full((rows,), V, dtype=torch.int32, device=DEV), **on)
+            assert torch.equal(again, token) and torch.equal(prob2, prob)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sample_long_top_k(b, dtype):
+    """More tokens than the short list takes, with and without top-p behind them."""
+    g = gen(77)
+    rows, V = 20, 30001
+    z = (2 * torch.randn((rows, V), generator=g)).to(dtype)
+    z[1] = z[1].round()
+    for k, p in ((513, 1.0), (5000, 0.9), (29999, 0.99), (513, 0.2)):
+        u = torch.rand(rows, generator=g)
+        s = dict(top_k=torch.full((rows,), k, dtype=torch.int32), top_p=torch.full((rows,), p))
+        token, prob = torch.empty(rows, dtype=torch.int32, device=DEV), torch.empty(rows, device=DEV)
+        b.elmo_sample(z.to(DEV), u.to(DEV), token, prob_out=prob, **{n: v.to(DEV) for n, v in s.items()})
+        check_tokens(z, u, token.cpu(), prob.cpu(), **s)
+
+
 def test_sample_shares_of_many_draws(b):
     V, n = 40, 20000
     z = torch.randn(V, generator=gen(3))

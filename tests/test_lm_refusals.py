@@ -133,6 +133,14 @@ def test_calls_without_rows_do_nothing(b):
     _distill(b, rows=0, z=None)
 
 
+def test_missing_or_small_workspaces_are_refused(b):
+    for call, kw in ((_sample, dict(V=1 << 17, zs=1 << 17, rows=2)), (_distill, dict(V=1 << 17, zs=1 << 17, rows=2))):
+        need = (b.elmo_sample_bytes if call is _sample else b.elmo_distill_bytes)(2, 1 << 17)
+        assert need > 0
+        for ws, n in ((None, 0), (P, need - 1), (P + 64, need)):
+            assert "workspace" in refused(b, -1, call, b, ws=ws, n=n, **kw)
+
+
 def test_workspaces(b):
     assert b.elmo_rms_norm_backward_bytes(0, 64) == 0 and b.elmo_rms_norm_backward_bytes(3, 64) == 3 * 64 * 4
     big = b.elmo_rms_norm_backward_bytes(1 << 20, 4096)
