@@ -225,7 +225,7 @@ void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t o
  *    same bits every time.
  * --------------------------------------------------------------------------------------------- */
 
-/* Root-mean-square norm of rows of d elements (1 <= d <= 65536), behind a residual's addition:
+/* Root-mean-square norm of rows of d elements (1 <= d <= 16384), behind a residual's addition:
  *   h = x + residual (x alone if residual is NULL),  y = weight * h / sqrt(mean(h^2) + eps)
  * weight [d] (NULL = ones) has a dtype of its own.  sum_out (NULL = not wanted; needs a residual)
  * receives h rounded to dtype, y is formed from the unrounded h.  y_dtype: ELMO_BF16 or ELMO_FP32, or 8 bits

@@ -20,7 +20,7 @@ using elmo::check_launch;
 using elmo::fail;
 
 constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;      // rows of a launch
-constexpr int kNormMostD = 65536;                          // what a workgroup's registers hold
+constexpr int kNormMostD = 16384;                          // what a workgroup's registers hold
 
 int check_rows(const char* what, int64_t rows, int64_t n, int64_t most) {
   if (rows < 0 || rows > kMostRows) return fail(-1, "%s: rows = %lld outside [0, 2^31)", what, (long long)rows);
@@ -40,14 +40,13 @@ int check_aligned(const char* what, const void* p, int dtype) {
 }
 #define ELMO_TRY(call) do { if (int rc_ = (call)) return rc_; } while (0)
 
-// ---- norm: waves of a row and octets of a lane.  One wave keeps a row of up to 4096 elements without a barrier; where the rows are
-// too few to fill the chip that way, four waves share one and each has a quarter of the work.
+// ---- norm: waves of a row and octets of a lane.  Short rows a wave each, without a barrier; longer ones four waves, with as much in flight in fewer
+// registers (16384 rows of 1024 BF16 -> INT8: 24.6 us with one wave, 31.0 with four; of 4096: 104 and 97; 1 row of 4096: 9.1 and 4.4).
 struct RowShape { int wpr, steps; };
-RowShape norm_shape(int64_t rows, int d) {
-  const bool many = rows >= 4096;
-  if (d <= (many ? 4096 : 512)) return {1, (d + 511) / 512};
+RowShape norm_shape(int d) {
+  if (d <= 1024) return {1, (d + 511) / 512};
   if (d <= 8192) return {4, (d + 2047) / 2048};
-  return {16, (d + 8191) / 8192};
+  return {16, 2};
 }
 int pow2_at_least(int n) { int p = 1; while (p < n) p *= 2; return p; }
 
@@ -56,12 +55,12 @@ template <class T, int OUT, int WPR, int S> void launch_norm(const elmo::NormArg
   elmo::k_rms_norm<T, OUT, WPR, S><<<(unsigned)((a.rows + rpg - 1) / rpg), threads, 0, st>>>(a);
 }
 template <class T, int OUT> void launch_norm_shape(const elmo::NormArgs& a, hipStream_t st) {
-  const RowShape r = norm_shape(a.rows, a.d);
+  const RowShape r = norm_shape(a.d);
   const int s = pow2_at_least(r.steps);
 #define ELMO_NORM(W, S) if (r.wpr == W && s == S) return launch_norm<T, OUT, W, S>(a, st)
-  ELMO_NORM(1, 1); ELMO_NORM(1, 2); ELMO_NORM(1, 4); ELMO_NORM(1, 8);
+  ELMO_NORM(1, 1); ELMO_NORM(1, 2);
   ELMO_NORM(4, 1); ELMO_NORM(4, 2); ELMO_NORM(4, 4);
-  ELMO_NORM(16, 2); ELMO_NORM(16, 4); ELMO_NORM(16, 8);
+  ELMO_NORM(16, 2);
 #undef ELMO_NORM
 }
 template <class T> void launch_norm_out(const elmo::NormArgs& a, int out, hipStream_t st) {
@@ -71,25 +70,23 @@ template <class T> void launch_norm_out(const elmo::NormArgs& a, int out, hipStr
   else launch_norm_shape<T, elmo::OUT_INT8>(a, st);
 }
 
-// Backward: a team of waves keeps its columns' share of the weight gradient over all rows it takes.
-constexpr int kNormTeams = 1024;
-RowShape back_shape(int d) {
-  if (d <= 1024) return {1, (d + 511) / 512};
-  if (d <= 8192) return {4, (d + 2047) / 2048};
-  return {16, (d + 8191) / 8192};
+// Backward: a team of waves keeps its columns' share of the weight gradient over all rows it takes, and a workgroup leaves one share: 512 of them (16384 x
+// 4096 BF16: 107 us; 256: 136, 1024: 127).
+constexpr int kNormShares = 512;
+int back_shares(int64_t rows, int64_t d) {
+  const int64_t teams = d <= 1024 ? 4 : 1;               // of a workgroup
+  return (int)std::min<int64_t>((rows + teams - 1) / teams, kNormShares);
 }
-int back_teams(int64_t rows) { return (int)std::min<int64_t>(rows, kNormTeams); }
 template <class T, int WPR, int S> void launch_back(const elmo::NormBackArgs& a, hipStream_t st) {
-  constexpr int threads = elmo::norm_threads(WPR), rpg = threads / (64 * WPR);
-  elmo::k_rms_norm_back<T, WPR, S><<<(a.teams + rpg - 1) / rpg, threads, 0, st>>>(a);
+  elmo::k_rms_norm_back<T, WPR, S><<<a.shares, elmo::norm_threads(WPR), 0, st>>>(a);
 }
 template <class T> void launch_back_shape(const elmo::NormBackArgs& a, hipStream_t st) {
-  const RowShape r = back_shape(a.d);
+  const RowShape r = norm_shape(a.d);
   const int s = pow2_at_least(r.steps);
 #define ELMO_BACK(W, S) if (r.wpr == W && s == S) return launch_back<T, W, S>(a, st)
   ELMO_BACK(1, 1); ELMO_BACK(1, 2);
   ELMO_BACK(4, 1); ELMO_BACK(4, 2); ELMO_BACK(4, 4);
-  ELMO_BACK(16, 2); ELMO_BACK(16, 4); ELMO_BACK(16, 8);
+  ELMO_BACK(16, 2);
 #undef ELMO_BACK
 }
 
@@ -126,7 +123,7 @@ extern "C" int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t
 }
 
 extern "C" size_t elmo_rms_norm_backward_bytes(int64_t rows, int64_t d) {
-  return rows < 1 || d < 1 || d > kNormMostD ? 0 : (size_t)back_teams(rows) * (size_t)d * sizeof(float);
+  return rows < 1 || d < 1 || d > kNormMostD ? 0 : (size_t)back_shares(rows, d) * (size_t)d * sizeof(float);
 }
 
 extern "C" int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int64_t h_stride, int dtype, int64_t rows, int64_t d,
@@ -138,7 +135,7 @@ extern "C" int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const v
   if (!(eps >= 0.0f) || eps > 1e30f) return fail(-1, "eps must be >= 0 and finite (got %g)", (double)eps);
   ELMO_TRY(check_aligned("dweight", dweight, ELMO_FP32));
   hipStream_t st = (hipStream_t)hip_stream;
-  const int teams = back_teams(rows);
+  const int shares = back_shares(rows, d);
   if (rows > 0) {
     if (!dy || !h || !dh) return fail(-1, "dy, h and dh must not be NULL");
     ELMO_TRY(check_stride("dy_stride", dy_stride, d, rows));
@@ -154,13 +151,14 @@ extern "C" int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const v
       return fail(-1, "workspace missing or smaller than %zu bytes", elmo_rms_norm_backward_bytes(rows, d));
     if (dweight) ELMO_TRY(check_aligned("workspace", workspace, ELMO_FP32));
     const elmo::NormBackArgs a{dy, h, weight, dsum, dh, dweight ? (float*)workspace : nullptr, rows, dy_stride, h_stride, dsum_stride, dh_stride,
-                               (int)d, teams, eps, weight_dtype == ELMO_FP32};
+                               (int)d, shares, eps, weight_dtype == ELMO_FP32};
     if (dtype == ELMO_BF16) launch_back_shape<uint16_t>(a, st);
     else launch_back_shape<float>(a, st);
     ELMO_TRY(check_launch("k_rms_norm_back"));
   }
   if (!dweight) return 0;
-  elmo::k_norm_dweight<<<(unsigned)((d + 63) / 64), 64 * elmo::kDweightWaves, 0, st>>>((const float*)workspace, teams, (int)d, dweight);
+  elmo::k_norm_dweight<<<(unsigned)((d + elmo::kDweightCols - 1) / elmo::kDweightCols), elmo::kDweightThreads, 0, st>>>((const float*)workspace, shares,
+                                                                                                                       (int)d, dweight);
   return check_launch("k_norm_dweight");
 }
 

@@ -163,14 +163,14 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm(NormArgs a) {
 
 // Backward pass.  With g = w dy:
 //   dh = R (g - h R^2 mean(g h)) + dsum,   dw = sum over rows of R dy h.
-// A team of WPR waves takes every teams-th row and keeps its columns' share of dw in registers; the teams' shares go to `part`
-// ([teams, d] FP32) and are summed in a fixed order by k_norm_dweight: no atomics, the same bits every time.
+// A team of WPR waves keeps its columns' share of dw in registers over the rows that it takes; a workgroup's teams add theirs, and the workgroups' shares
+// go to `part` ([shares, d] FP32) and are summed in a fixed order by k_norm_dweight: no atomics, the same bits every time.
 struct NormBackArgs {
   const void *dy, *h, *w, *dsum;
   void* dh;
   float* part;                       // NULL: no weight gradient
   int64_t rows, dys, hs, dss, dhs;
-  int d, teams;
+  int d, shares;                     // shares: workgroups
   float eps;
   bool w32;
 };
@@ -180,8 +180,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm_back(NormBackArg
   constexpr int RPG = norm_threads(WPR) / (64 * WPR);
   __shared__ f32x2 s_red[2][RPG][WPR];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in_row = wave % WPR, slot = wave / WPR;
-  const int team = blockIdx.x * RPG + slot;
-  if (WPR == 1 && team >= a.teams) return;
+  const int team = blockIdx.x * RPG + slot, teams = a.shares * RPG;
   const int c0 = (in_row * 64 + lane) * 8;
   constexpr int STEP = WPR * 512;
   float w[S][8], dw[S][8];
@@ -192,7 +191,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm_back(NormBackArg
     for (int i = 0; i < 8; ++i) dw[s][i] = 0.0f;
   }
   int phase = 0;
-  for (int64_t row = team; row < a.rows; row += a.teams, phase ^= 1) {
+  for (int64_t row = team; row < a.rows; row += teams, phase ^= 1) {
     const T* dy = (const T*)a.dy + row * a.dys;
     const T* h = (const T*)a.h + row * a.hs;
     Octet<T> go[S], ho[S], so[S];
@@ -245,30 +244,48 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm_back(NormBackArg
       }
     }
   }
-  if (a.part) {
+  if (!a.part) return;
+  if constexpr (RPG > 1) {           // (WPR 1: lane for lane the same columns)
+    __shared__ float s_dw[RPG - 1][S * 8][64];
+    if (slot) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int c = c0 + s * STEP;
-      if (c < a.d) store_octet(a.part + (int64_t)team * a.d + c, a.d - c, dw[s]);
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_dw[slot - 1][8 * s + i][lane] = dw[s][i];
     }
+    __syncthreads();
+    if (slot) return;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int t = 0; t < RPG - 1; ++t) dw[s][i] += s_dw[t][8 * s + i][lane];
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const int c = c0 + s * STEP;
+    if (c < a.d) store_octet(a.part + (int64_t)blockIdx.x * a.d + c, a.d - c, dw[s]);
   }
 }
 
-// dw[c] = sum of the teams' shares: 64 columns a workgroup, its 16 waves take every 16th team, then their sums in order.
-constexpr int kDweightWaves = 16;
-__global__ __launch_bounds__(64 * kDweightWaves) static void k_norm_dweight(const float* __restrict__ part, int teams, int d, float* __restrict__ dw) {
-  __shared__ float s[kDweightWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+// dw[c] = sum of the workgroups' shares: 16 columns a workgroup, 64 threads for each of them that take every 64th share, then their sums in order.
+constexpr int kDweightCols = 16, kDweightLanes = 64, kDweightThreads = kDweightCols * kDweightLanes;
+__global__ __launch_bounds__(kDweightThreads) static void k_norm_dweight(const float* __restrict__ part, int shares, int d, float* __restrict__ dw) {
+  __shared__ float s[kDweightLanes][kDweightCols + 1];
+  const int col = threadIdx.x % kDweightCols, from = threadIdx.x / kDweightCols, c = blockIdx.x * kDweightCols + col;
   float v = 0.0f;
   if (c < d)
-    for (int t = wave; t < teams; t += kDweightWaves) v += part[(int64_t)t * d + c];
-  s[wave][lane] = v;
+#pragma unroll 4
+    for (int t = from; t < shares; t += kDweightLanes) v += part[(int64_t)t * d + c];
+  s[from][col] = v;
   __syncthreads();
-  if (wave == 0 && c < d) {
 #pragma unroll
-    for (int i = 1; i < kDweightWaves; ++i) v += s[i][lane];
-    dw[c] = v;
+  for (int n = kDweightLanes / 2; n >= 1; n /= 2) {
+    if (from < n) s[from][col] = v += s[from + n][col];
+    __syncthreads();
   }
+  if (from == 0 && c < d) dw[c] = v;
 }
 
 }  // namespace elmo

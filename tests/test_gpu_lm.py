@@ -56,7 +56,7 @@ def close(got, want, tol, what):
 
 
 # ------------------------------------------------------------------ norm
-NORM_SHAPES = [(1, 1), (1, 768), (3, 7), (5, 8), (2, 511), (7, 513), (4, 1000), (3, 2049), (2, 4096), (2, 4104), (1, 8193), (3, 20011), (1, 65536),
+NORM_SHAPES = [(1, 1), (1, 768), (3, 7), (5, 8), (2, 511), (7, 513), (4, 1000), (3, 2049), (2, 4096), (2, 4104), (1, 8193), (3, 12011), (1, 16384),
                (4100, 65), (4099, 1030), (4097, 4096)]
 
 
@@ -126,7 +126,7 @@ def test_norm_rows_that_hold_infinities_and_nan(b):
     assert bool(torch.isnan(y[1]).all()) and bool(torch.isfinite(y[[0, 5]]).all())
 
 
-@pytest.mark.parametrize("rows,d", [(0, 64), (1, 1), (1, 768), (3, 9), (2, 1025), (5, 4096), (2, 8200), (1030, 100), (1500, 1001), (2100, 2048), (1, 65536)])
+@pytest.mark.parametrize("rows,d", [(0, 64), (1, 1), (1, 768), (3, 9), (2, 1025), (5, 4096), (2, 8200), (1030, 100), (1500, 1001), (2100, 2048), (1, 16384), (700, 9001)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_norm_backward(b, rows, d, dtype):
     g = gen(rows + 31 * d)

@@ -106,7 +106,7 @@ NAN = float("nan")
 
 @pytest.mark.parametrize("call,code,kw", [
     (_norm, -2, dict(dt=1)), (_norm, -2, dict(dt=7)), (_norm, -2, dict(yt=9)), (_norm, -2, dict(w=P, wt=1)), (_norm, -1, dict(rows=-1)),
-    (_norm, -1, dict(rows=1 << 31)), (_norm, -1, dict(d=0)), (_norm, -1, dict(d=65537)), (_norm, -1, dict(eps=-1.0)), (_norm, -1, dict(eps=NAN)),
+    (_norm, -1, dict(rows=1 << 31)), (_norm, -1, dict(d=0)), (_norm, -1, dict(d=16385)), (_norm, -1, dict(eps=-1.0)), (_norm, -1, dict(eps=NAN)),
     (_norm, -1, dict(x=None)), (_norm, -1, dict(y=None)), (_norm, -1, dict(xs=63)), (_norm, -1, dict(ys=-64)), (_norm, -1, dict(r=P, rs=10)),
     (_norm, -1, dict(s=P, ss=64)), (_norm, -1, dict(yt=3)), (_norm, -1, dict(sc=P)), (_norm, -1, dict(x=P + 1)), (_norm, -1, dict(xs=1 << 41)),
     (_back, -2, dict(dt=3)), (_back, -1, dict(d=70000)), (_back, -1, dict(dw=P)), (_back, -1, dict(dw=P, ws=P, n=100)), (_back, -1, dict(dh=None)),
@@ -142,7 +142,7 @@ def test_missing_or_small_workspaces_are_refused(b):
 
 
 def test_workspaces(b):
-    assert b.elmo_rms_norm_backward_bytes(0, 64) == 0 and b.elmo_rms_norm_backward_bytes(3, 64) == 3 * 64 * 4
+    assert b.elmo_rms_norm_backward_bytes(0, 64) == 0 and 64 * 4 <= b.elmo_rms_norm_backward_bytes(3, 64) <= 3 * 64 * 4
     big = b.elmo_rms_norm_backward_bytes(1 << 20, 4096)
     assert 0 < big <= 4096 * 4096 * 4                        # it does not grow with the rows
     for fn in (b.elmo_sample_bytes, b.elmo_distill_bytes):
