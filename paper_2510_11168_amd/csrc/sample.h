@@ -11,7 +11,7 @@
 // weights' arithmetic (some twenty FP64 and integer instructions each).  What is done, by the row's settings:
 //   top_k <= 512   the k-th largest of the threads' maxima bounds the k-th token from below; the few tokens above it go to a list in LDS,
 //                  which is sorted, filtered and drawn from: two readings, no weights but the list's;
-//   top_p, top_k   counts and weights over bins of 1/32 octave of weight, then the tokens of the bin in which the filter ends, sorted (a bin
+//   top_p, top_k   counts and weights over bins of 1/64 octave of weight, then the tokens of the bin in which the filter ends, sorted (a bin
 //                  that holds too many: a radix search over their places); three readings, four with both;
 //   BF16           in place of the bins, counts of the logits' codes: a weight is computed once a code, and the place at which a filter ends
 //                  is a code and a number of tokens that have it;
@@ -26,7 +26,7 @@ namespace elmo {
 constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleShortK = 512;             // largest top_k that goes by the threads' maxima
 constexpr int kSampleList = 4096;              // places of the list in LDS; segments of a row
-constexpr int kSampleBins = 2048;              // 1/32 octave each: 64 octaves, more than weights have
+constexpr int kSampleBins = 2048;              // 1/64 octave each, the last one everything below 2^-32 of the largest weight
 constexpr uint32_t kKeyNone = 0x007FFFFFu;     // key of -infinity: never kept
 
 struct SampleArgs {
@@ -71,7 +71,7 @@ struct Weigh {
     return (uint64_t)__double_as_longlong(w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52: rounded to a whole number
   }
   __device__ inline uint64_t operator()(float z) const { int n; return (*this)(z, n); }
-  __device__ inline int bin(int n) const { return min(-n >> 3, kSampleBins - 1); }        // 0: the largest weights
+  __device__ inline int bin(int n) const { return min(-n >> 2, kSampleBins - 1); }        // 0: the largest weights
 };
 
 template <class T> __device__ inline T lowest();                       // -infinity
@@ -182,7 +182,7 @@ struct SampleCodes {
   uint32_t count[kCodesEach * kSampleThreads];
 };
 
-// One row in the hands of a workgroup.
+// One row in the hands of a workgroup.  Everything inlined into the kernels: called, its state would lie in scratch memory and LDS would be reached through flat addresses.
 template <class T> struct Sampler {
   static constexpr int NT = kSampleThreads;
   const SampleArgs& a;
@@ -197,12 +197,12 @@ template <class T> struct Sampler {
   float low = -__builtin_inff();                                 // smallest kept logit,
   uint32_t last = ~0u;                                           // and of those equal to it the last kept index
 
-  __device__ inline Sampler(const SampleArgs& args, SampleLds& lds, int64_t r)
+  __device__ __forceinline__ Sampler(const SampleArgs& args, SampleLds& lds, int64_t r)
       : a(args), l(lds), row(r), octets((args.V + 7) >> 3), per(((octets + 63) / 64 + kSampleList - 1) / kSampleList),
         segments((int)(((octets + 63) / 64 + per - 1) / per)), tid(threadIdx.x), lane(threadIdx.x & 63), wave(threadIdx.x >> 6),
         z((const T*)args.z + r * args.zs), rs(settings_of(args, r)) {}
 
-  __device__ inline void load8(int64_t o, float (&f)[8]) const {
+  __device__ __forceinline__ void load8(int64_t o, float (&f)[8]) const {
     const Octet<T> oc = load_octet(z + o * 8, a.V - o * 8, lowest<T>());
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = oc[i];
@@ -211,19 +211,19 @@ template <class T> struct Sampler {
       for (int i = 0; i < 8; ++i) f[i] = f[i] == __builtin_inff() ? 0.0f : -__builtin_inff();
     }
   }
-  static __device__ inline float max8(const float (&f)[8]) {
+  static __device__ __forceinline__ float max8(const float (&f)[8]) {
     return fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])), fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
   }
-  __device__ inline void answer(int64_t token, float prob) const {
+  __device__ __forceinline__ void answer(int64_t token, float prob) const {
     a.token[row] = (int32_t)token;
     if (a.prob) a.prob[row] = prob;
   }
-  __device__ inline uint64_t number(uint64_t all) const {        // u of the kept weight
+  __device__ __forceinline__ uint64_t number(uint64_t all) const {        // u of the kept weight
     const uint64_t want = (uint64_t)(rs.u * (double)all);
     return want >= all ? all - 1 : want;
   }
   // A thread's largest logit among the octets [from, to).
-  __device__ inline float largest(int64_t from, int64_t to) const {
+  __device__ __forceinline__ float largest(int64_t from, int64_t to) const {
     float m = -__builtin_inff();
 #pragma unroll 8
     for (int64_t o = from + tid; o < to; o += NT) {
@@ -234,7 +234,7 @@ template <class T> struct Sampler {
     return m;
   }
   // The row's weights, once its largest logit is known (> -infinity).  Holds a barrier.
-  __device__ inline void set_max(float M) {
+  __device__ __forceinline__ void set_max(float M) {
     infinite = M == __builtin_inff();
     if (tid < 256) l.root[tid] = exp_series(tid * (kLn2 / 256));
     if (tid == 0) l.n = 0;
@@ -243,7 +243,7 @@ template <class T> struct Sampler {
     __syncthreads();
   }
   // Appends the logits >= from that keep() names to the list.
-  template <class F> __device__ inline void collect(float from, F&& keep) {
+  template <class F> __device__ __forceinline__ void collect(float from, F&& keep) {
 #pragma unroll 4
     for (int64_t o = tid; o < octets; o += NT) {
       float f[8];
@@ -259,7 +259,7 @@ template <class T> struct Sampler {
     }
     __syncthreads();
   }
-  __device__ inline void order_list(int n) {
+  __device__ __forceinline__ void order_list(int n) {
     if (n <= kSampleCount) return rank_falling(l.list, l.count, n, tid);
     int size = 2;
     while (size < n) size *= 2;
@@ -268,7 +268,7 @@ template <class T> struct Sampler {
   }
   // found[0] = the place at which the list's n tokens, behind `above` tokens of weight mass_above, first make up `want` tokens or weight; found[1]
   // = the weight down to it.  Changes count.
-  __device__ inline void cut_list(int n, bool by_mass, uint64_t want, uint64_t above, uint64_t mass_above) {
+  __device__ __forceinline__ void cut_list(int n, bool by_mass, uint64_t want, uint64_t above, uint64_t mass_above) {
     order_list(n);
     uint64_t w[4], sum = 0, whole;                       // four a thread
 #pragma unroll
@@ -285,17 +285,19 @@ template <class T> struct Sampler {
   }
   // Into found: the bin in which tokens or weight, `before` ahead of this thread's two bins with c0 and c1, first make up `want`; what lies ahead of it; the
   // weight ahead of it.
-  __device__ inline void find_bin(uint64_t want, uint64_t before, uint64_t c0, uint64_t c1, uint64_t mass_before, uint64_t m0) {
+  __device__ __forceinline__ void find_bin(uint64_t want, uint64_t before, uint64_t c0, uint64_t c1, uint64_t mass_before, uint64_t m0) {
     __syncthreads();
     if (before < want && before + c0 >= want) { l.found[0] = 2 * tid; l.found[1] = before; l.found[2] = mass_before; }
     if (before + c0 < want && before + c0 + c1 >= want) { l.found[0] = 2 * tid + 1; l.found[1] = before + c0; l.found[2] = mass_before + m0; }
     __syncthreads();
   }
   // A bound below a bin's logits, with room for the rounding of y, so that octets below it are passed over.
-  __device__ inline float bin_floor(int bin) const { return (float)(weigh.M + (-8.0 * bin - 9.0) / weigh.k) - 1e-5f * fabsf((float)weigh.M); }
+  __device__ __forceinline__ float bin_floor(int bin) const {
+    return bin == kSampleBins - 1 ? -__builtin_inff() : (float)(weigh.M + (-4.0 * bin - 5.0) / weigh.k) - 1e-5f * fabsf((float)weigh.M);
+  }
 
   // ---- top_k <= 512: bound, list, filters, draw.  False: the list does not hold what lies above the bound.
-  __device__ inline bool short_list(float mine) {
+  __device__ __forceinline__ bool short_list(float mine) {
     const float M = (float)weigh.M;
     if (rs.k == 1) {
       uint32_t first = ~0u;                              // the largest logit's first place
@@ -380,7 +382,7 @@ template <class T> struct Sampler {
   }
 
   // ---- weights (and counts) over bins, of the octets [from, to)
-  __device__ inline void fill_bins(int64_t from, int64_t to, bool by_count) {
+  __device__ __forceinline__ void fill_bins(int64_t from, int64_t to, bool by_count) {
     for (int i = tid; i < kSampleBins; i += NT) {
       l.mass[i] = 0;
       l.count[i] = 0;
@@ -403,12 +405,12 @@ template <class T> struct Sampler {
     __syncthreads();
   }
 
-  __device__ inline void set_edge(uint64_t place) {
+  __device__ __forceinline__ void set_edge(uint64_t place) {
     low = of_key(place >> 32);
     last = ~(uint32_t)place;
   }
   // The filter's end, from the bin in found.  Returns the weight down to it.
-  __device__ inline uint64_t end_in_bin(bool by_mass, uint64_t want) {
+  __device__ __forceinline__ uint64_t end_in_bin(bool by_mass, uint64_t want) {
     const int bin = (int)l.found[0];
     uint64_t above = l.found[1], mass_above = l.found[2];
     if (tid == 0) l.n = 0;
@@ -463,7 +465,7 @@ template <class T> struct Sampler {
   }
 
   // Weights of an octet's kept tokens, and their sum.
-  __device__ inline uint64_t kept8(int64_t o, uint64_t (&w)[8]) const {
+  __device__ __forceinline__ uint64_t kept8(int64_t o, uint64_t (&w)[8]) const {
     uint64_t sum = 0;
     float f[8];
     const bool in = o < octets;
@@ -484,7 +486,7 @@ template <class T> struct Sampler {
     return sum;
   }
   // ---- the token, from the segments' kept weight in list
-  __device__ inline void draw() {
+  __device__ __forceinline__ void draw() {
     uint64_t w4[4], sum = 0, all;
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum += w4[i] = 4 * tid + i < segments ? l.list[4 * tid + i] : 0;
@@ -513,12 +515,12 @@ template <class T> struct Sampler {
   }
 
   // ---- BF16, by codes.  False: not this row.
-  __device__ inline int slot(uint32_t code, int base) const {    // negative or beyond kCodes: none
+  __device__ __forceinline__ int slot(uint32_t code, int base) const {    // negative or beyond kCodes: none
     const int i = (int)(code & 0x7FFF) - base;
     const int s = code & 0x8000 ? kCodeHalf + i : kCodeHalf - 1 - i;
     return (uint32_t)i < (uint32_t)kCodeHalf ? s : -1;
   }
-  __device__ inline bool by_code(SampleCodes* c) {
+  __device__ __forceinline__ bool by_code(SampleCodes* c) {
     if (infinite) return false;
     const float bottom = (float)(weigh.M + weigh.least / weigh.k);       // (-infinity at a temperature of infinity)
     const uint32_t wide = f2u(fmaxf(fabsf((float)weigh.M), fminf(fabsf(bottom), 3.3e38f))) >> 23;   // exponents up to this one
@@ -715,7 +717,7 @@ template <class T> struct Sampler {
   }
 
   // ---- a row by one workgroup
-  __device__ inline void whole(SampleCodes* codes) {
+  __device__ __forceinline__ void whole(SampleCodes* codes) {
     float mine = largest(0, octets), M = wave_max(mine);
     if (lane == 0) l.max[wave] = M;
     __syncthreads();
@@ -763,20 +765,20 @@ template <class T> struct Sampler {
   }
 
   // ---- a row by several: this workgroup's segments [s0, s1)
-  __device__ inline SampleWs* shared_state() const { return (SampleWs*)(a.ws + row * kSampleRowBytes); }
-  __device__ inline void my_segments(int& s0, int& s1) const {
+  __device__ __forceinline__ SampleWs* shared_state() const { return (SampleWs*)(a.ws + row * kSampleRowBytes); }
+  __device__ __forceinline__ void my_segments(int& s0, int& s1) const {
     const int each = (segments + a.parts - 1) / a.parts, part = (int)(blockIdx.x % a.parts);
     s0 = min(segments, part * each);
     s1 = min(segments, s0 + each);
   }
   // The row's largest logit from its parts'; false where there is nothing for the split form to do.
-  __device__ inline bool split_max() {
+  __device__ __forceinline__ bool split_max() {
     const float M = wave_max(lane < a.parts ? shared_state()->max[lane] : -__builtin_inff());
     if (M == -__builtin_inff() || rs.k < a.V) return false;       // (a greedy row has k = 1: the last launch takes it whole)
     set_max(M);
     return true;
   }
-  __device__ inline void part_max() {
+  __device__ __forceinline__ void part_max() {
     SampleWs* ws = shared_state();
     const int part = (int)(blockIdx.x % a.parts);
     int s0, s1;
@@ -791,7 +793,7 @@ template <class T> struct Sampler {
       if (lane == 0 && part == 0) ws->n = 0;
     }
   }
-  __device__ inline void part_bins() {
+  __device__ __forceinline__ void part_bins() {
     if (rs.p >= 1.0 || !split_max()) return;
     int s0, s1;
     my_segments(s0, s1);
@@ -800,7 +802,7 @@ template <class T> struct Sampler {
       if (l.mass[i]) atomicAdd((unsigned long long*)&shared_state()->mass[i], (unsigned long long)l.mass[i]);
   }
   // Into found: the bin in which top-p ends.  Returns the weight that it asks for.
-  __device__ inline uint64_t split_bin() {
+  __device__ __forceinline__ uint64_t split_bin() {
     const SampleWs* ws = shared_state();
     uint64_t total;
     const uint64_t m0 = ws->mass[2 * tid], m1 = ws->mass[2 * tid + 1];
@@ -808,7 +810,7 @@ template <class T> struct Sampler {
     find_bin(want, mass_before, m0, m1, mass_before, m0);
     return want;
   }
-  __device__ inline void part_sums() {
+  __device__ __forceinline__ void part_sums() {
     if (!split_max()) return;
     SampleWs* ws = shared_state();
     int bin = kSampleBins, s0, s1;
@@ -845,7 +847,7 @@ template <class T> struct Sampler {
       if (lane == 0) ws->segment[s] = sum;
     }
   }
-  __device__ inline void split_draw(SampleCodes* codes) {
+  __device__ __forceinline__ void split_draw(SampleCodes* codes) {
     const SampleWs* ws = shared_state();
     const int n = (int)min(ws->n, (uint32_t)kSampleList + 1);
     if (n > kSampleList || !split_max()) return whole(codes);
