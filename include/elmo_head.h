@@ -219,10 +219,12 @@ void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t o
  *    Rows need no alignment beyond their elements'.  Nothing between rows is written.
  *  - Values are ELMO_BF16 or ELMO_FP32 as the dtype argument says; sums are FP32 or wider, every
  *    output is rounded once, to nearest even (overflow to infinity, NaN kept).
- *  - A call with no rows is a no-op.  Workspaces are scratch of the call: two calls that may
+ *  - All pointers are device pointers owned by the caller.  A call with no rows is a no-op.  Workspaces are scratch of the call: two calls that may
  *    overlap in time (streams, captured graphs) need one each.
- *  - Only kernels are enqueued: calls can be captured into a HIP graph.  The same call gives the
- *    same bits every time.
+ *  - Only kernels are enqueued, so after one ordinary call of its kind a call can be captured into
+ *    a HIP graph.  The same call gives the same bits every time.
+ *  - A launch takes less than 2^32 work-items: 2^22 rows of elmo_sample, 2^23 of elmo_distill, 2^24 of
+ *    elmo_rms_norm (2^26 of at most 1024 columns); more are refused.
  * --------------------------------------------------------------------------------------------- */
 
 /* Root-mean-square norm of rows of d elements (1 <= d <= 16384), behind a residual's addition:
@@ -233,7 +235,7 @@ void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t o
  *   ELMO_INT8:      y = round(127 p / m),       scale = m / (127 sqrt(mean(h^2) + eps))
  *   ELMO_FP8_E4M3:  y = round_E4M3(448 p / m),  scale = m / (448 sqrt(mean(h^2) + eps))
  * so that y * scale is the norm; the quotient is p * (127 * (1 / m)), p exact and three FP64 roundings.  A row of zeros gives zeros and scale 0; a row that holds an infinity or NaN, or squares beyond FP32,
- * gives zeros and scale NaN.  sum_out may be x or residual, y may be x or sum_out's place, where address, stride and dtype are the same. */
+ * gives zeros and scale NaN.  sum_out may be x or residual, and y the other of the two, where address, stride and dtype are the same. */
 int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int64_t d, const void* residual,
                   int64_t residual_stride, const void* weight, int weight_dtype, float eps, void* sum_out,
                   int64_t sum_stride, void* y, int64_t y_stride, int y_dtype, float* scale_out, void* hip_stream);
@@ -267,7 +269,7 @@ int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, co
  * Weights are whole multiples of 2^-F of the largest, F = min(50, 62 - ceil(log2 V)), computed in FP64 (a token below half of that
  * is never drawn), and their sums are exact: the token does not depend on how a row is split.
  * idx_out [rows]: the token, -1 where a row has none; prob_out [rows] (NULL = not wanted): its share of the kept weight, 0 where there
- * is none.  workspace: elmo_sample_bytes(rows, V) bytes, 256-byte aligned (NULL if that is 0). */
+ * is none.  workspace: elmo_sample_bytes(rows, V) bytes, 256-byte aligned (NULL if that is 0, and with top_k). */
 size_t elmo_sample_bytes(int64_t rows, int64_t V);
 int elmo_sample(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const float* u,
                 const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* idx_out,

@@ -361,7 +361,7 @@ def elmo_sample(logits, u, idx_out, *, temperature=None, top_k=None, top_p=None,
     ip, _ = _vector("idx_out", idx_out, _ONLY_INT32, rows)
     qp, _ = _vector("prob_out", prob_out, _ONLY_FP32, rows)
     _call(_lib.elmo_sample, (zp, zs, dtype, rows, V, up, tp, kp, pp, mp, ip, qp), (logits, u, idx_out, temperature, top_k, top_p, min_p, prob_out),
-          stream, workspace, elmo_sample_bytes(rows, V))
+          stream, workspace, elmo_sample_bytes(rows, V) if top_k is None else 0)
 
 
 def elmo_distill_bytes(rows, V) -> int:

@@ -19,7 +19,7 @@ namespace {
 using elmo::check_launch;
 using elmo::fail;
 
-constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;      // rows of a launch
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;
 constexpr int kNormMostD = 16384;                          // what a workgroup's registers hold
 
 int check_rows(const char* what, int64_t rows, int64_t n, int64_t most) {
@@ -38,6 +38,21 @@ int check_aligned(const char* what, const void* p, int dtype) {
   if ((uintptr_t)p & (size - 1)) return fail(-1, "%s must be aligned to its elements", what);
   return 0;
 }
+// Work-items of a launch are counted in 32 bits.
+int check_grid(const char* what, int64_t workgroups, int threads) {
+  if (workgroups > (int64_t)UINT32_MAX / threads) return fail(-1, "%s: more rows than one launch takes", what);
+  return 0;
+}
+// Opt in to more than 64 KiB of LDS, once for each kernel and device, whichever host thread comes first.
+constexpr int kMostDevices = 64;
+template <class Kernel> int raise_lds(Kernel* kernel, int bytes, std::once_flag (&once)[kMostDevices], hipError_t (&rc)[kMostDevices]) {
+  int dev = -1;
+  ELMO_HIP(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMostDevices) return fail(-3, "device ordinal %d outside [0, %d)", dev, kMostDevices);
+  std::call_once(once[dev], [&] { rc[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+  if (rc[dev] != hipSuccess) return fail(-3, "hipFuncSetAttribute failed: %s", hipGetErrorString(rc[dev]));
+  return 0;
+}
 #define ELMO_TRY(call) do { if (int rc_ = (call)) return rc_; } while (0)
 
 // ---- norm: waves of a row and octets of a lane.  Short rows a wave each, without a barrier; longer ones four waves, with as much in flight in fewer
@@ -50,24 +65,26 @@ RowShape norm_shape(int d) {
 }
 int pow2_at_least(int n) { int p = 1; while (p < n) p *= 2; return p; }
 
-template <class T, int OUT, int WPR, int S> void launch_norm(const elmo::NormArgs& a, hipStream_t st) {
+template <class T, int OUT, int WPR, int S> int launch_norm(const elmo::NormArgs& a, hipStream_t st) {
   constexpr int threads = elmo::norm_threads(WPR), rpg = threads / (64 * WPR);
+  ELMO_TRY(check_grid("elmo_rms_norm", (a.rows + rpg - 1) / rpg, threads));
   elmo::k_rms_norm<T, OUT, WPR, S><<<(unsigned)((a.rows + rpg - 1) / rpg), threads, 0, st>>>(a);
+  return check_launch("k_rms_norm");
 }
-template <class T, int OUT> void launch_norm_shape(const elmo::NormArgs& a, hipStream_t st) {
+template <class T, int OUT> int launch_norm_shape(const elmo::NormArgs& a, hipStream_t st) {
   const RowShape r = norm_shape(a.d);
   const int s = pow2_at_least(r.steps);
 #define ELMO_NORM(W, S) if (r.wpr == W && s == S) return launch_norm<T, OUT, W, S>(a, st)
   ELMO_NORM(1, 1); ELMO_NORM(1, 2);
   ELMO_NORM(4, 1); ELMO_NORM(4, 2); ELMO_NORM(4, 4);
-  ELMO_NORM(16, 2);
 #undef ELMO_NORM
+  return launch_norm<T, OUT, 16, 2>(a, st);
 }
-template <class T> void launch_norm_out(const elmo::NormArgs& a, int out, hipStream_t st) {
-  if (out == ELMO_BF16) launch_norm_shape<T, elmo::OUT_BF16>(a, st);
-  else if (out == ELMO_FP32) launch_norm_shape<T, elmo::OUT_FP32>(a, st);
-  else if (out == ELMO_FP8_E4M3) launch_norm_shape<T, elmo::OUT_E4M3>(a, st);
-  else launch_norm_shape<T, elmo::OUT_INT8>(a, st);
+template <class T> int launch_norm_out(const elmo::NormArgs& a, int out, hipStream_t st) {
+  if (out == ELMO_BF16) return launch_norm_shape<T, elmo::OUT_BF16>(a, st);
+  if (out == ELMO_FP32) return launch_norm_shape<T, elmo::OUT_FP32>(a, st);
+  if (out == ELMO_FP8_E4M3) return launch_norm_shape<T, elmo::OUT_E4M3>(a, st);
+  return launch_norm_shape<T, elmo::OUT_INT8>(a, st);
 }
 
 // Backward: a team of waves keeps its columns' share of the weight gradient over all rows it takes, and a workgroup leaves one share: 512 of them (16384 x
@@ -117,9 +134,7 @@ extern "C" int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t
   ELMO_TRY(check_aligned("scale_out", scale_out, ELMO_FP32));
   const elmo::NormArgs a{x, residual, weight, sum_out, y, scale_out, rows, x_stride, residual_stride, sum_stride, y_stride, (int)d, eps,
                          weight_dtype == ELMO_FP32};
-  if (dtype == ELMO_BF16) launch_norm_out<uint16_t>(a, y_dtype, (hipStream_t)hip_stream);
-  else launch_norm_out<float>(a, y_dtype, (hipStream_t)hip_stream);
-  return check_launch("k_rms_norm");
+  return dtype == ELMO_BF16 ? launch_norm_out<uint16_t>(a, y_dtype, (hipStream_t)hip_stream) : launch_norm_out<float>(a, y_dtype, (hipStream_t)hip_stream);
 }
 
 extern "C" size_t elmo_rms_norm_backward_bytes(int64_t rows, int64_t d) {
@@ -166,14 +181,11 @@ namespace {
 template <class O, int TM, int TN, int FM, int FN, int NST, bool ASYNC> int launch_int8_as(const elmo::Int8Args& p, hipStream_t st) {
   constexpr int smem = elmo::int8_smem<TM, TN, NST>();
   static_assert(smem <= 160 * 1024, "LDS of the tiles");
-  // once per process and instantiation, whichever host thread comes first
-  static std::once_flag once;
-  static hipError_t attr_rc = hipSuccess;
-  std::call_once(once, [] {
-    attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&elmo::k_int8_tiles<O, TM, TN, FM, FN, NST, ASYNC>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  });
-  if (attr_rc != hipSuccess) return fail(-3, "hipFuncSetAttribute(k_int8_tiles) failed: %s", hipGetErrorString(attr_rc));
   const int tiles_m = (p.M + TM - 1) / TM, tiles_n = (p.N + TN - 1) / TN;
+  ELMO_TRY(check_grid("elmo_int8_matmul", (int64_t)tiles_m * tiles_n, elmo::int8_threads<TM, TN, FM, FN>()));
+  static std::once_flag once[kMostDevices];
+  static hipError_t attr[kMostDevices];
+  ELMO_TRY(raise_lds(&elmo::k_int8_tiles<O, TM, TN, FM, FN, NST, ASYNC>, smem, once, attr));
   elmo::k_int8_tiles<O, TM, TN, FM, FN, NST, ASYNC><<<tiles_m * tiles_n, elmo::int8_threads<TM, TN, FM, FN>(), smem, st>>>(p, tiles_m, tiles_n);
   return check_launch("k_int8_tiles");
 }
@@ -181,6 +193,7 @@ template <class O, int TM, int TN, int FM, int FN, int NST> int launch_int8_tile
   return aligned ? launch_int8_as<O, TM, TN, FM, FN, NST, true>(p, st) : launch_int8_as<O, TM, TN, FM, FN, 2, false>(p, st);
 }
 template <class O, int FM> int launch_int8_skinny(const elmo::Int8Args& p, hipStream_t st) {
+  ELMO_TRY(check_grid("elmo_int8_matmul", (p.N + 15) / 16, elmo::kSkinnyThreads));
   elmo::k_int8_skinny<O, FM><<<(unsigned)((p.N + 15) / 16), elmo::kSkinnyThreads, 0, st>>>(p);
   return check_launch("k_int8_skinny");
 }
@@ -196,7 +209,6 @@ template <class O> int launch_int8(elmo::Int8Args p, hipStream_t st) {
   if (p.N == 1) p.bs = 0;
   const auto tiles = [&](int t) { return (int64_t)((p.M + t - 1) / t) * ((p.N + t - 1) / t); };
   const auto rounds = [](int64_t n, int64_t slots) { return (n + slots - 1) / slots; };
-  if (tiles(64) > kMostRows) return fail(-1, "M x N = %d x %d is more than one launch takes", p.M, p.N);
   if (p.M <= 16 && (p.K >= 2048 || p.N <= 16384)) return launch_int8_skinny<O, 1>(p, st);
   if (p.M <= 32 && p.N <= 4096) return launch_int8_skinny<O, 2>(p, st);
   // (row offsets within a tile are formed from 24-bit factors)
@@ -246,17 +258,15 @@ template <class T, int STEP> int launch_sample_step(const elmo::SampleArgs& a, u
   constexpr int smem = elmo::sample_smem<T, STEP>();
   static_assert(smem + sizeof(elmo::SampleLds) <= 160 * 1024, "LDS of a row");
   if constexpr (smem > 0) {
-    static std::once_flag once;
-    static hipError_t attr_rc = hipSuccess;
-    std::call_once(once, [] {
-      attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(&elmo::k_sample<T, STEP>), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    });
-    if (attr_rc != hipSuccess) return fail(-3, "hipFuncSetAttribute(k_sample) failed: %s", hipGetErrorString(attr_rc));
+    static std::once_flag once[kMostDevices];
+    static hipError_t attr[kMostDevices];
+    ELMO_TRY(raise_lds(&elmo::k_sample<T, STEP>, smem, once, attr));
   }
   elmo::k_sample<T, STEP><<<grid, elmo::kSampleThreads, smem, st>>>(a);
   return check_launch("k_sample");
 }
 template <class T> int launch_sample(const elmo::SampleArgs& a, int64_t rows, hipStream_t st) {
+  ELMO_TRY(check_grid("elmo_sample", rows * a.parts, elmo::kSampleThreads));
   const unsigned one = (unsigned)rows, all = (unsigned)(rows * a.parts);
   if (a.parts == 1) return launch_sample_step<T, elmo::SAMPLE_WHOLE>(a, one, st);
   ELMO_TRY((launch_sample_step<T, elmo::SAMPLE_MAX>(a, all, st)));
@@ -284,11 +294,12 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
     ELMO_TRY(check_aligned("u, temperature, top_k, top_p, min_p, idx_out and prob_out", p, ELMO_FP32));
   int bits = 0;
   while (((int64_t)1 << bits) < V) ++bits;
-  const size_t need = elmo_sample_bytes(rows, V);
-  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return fail(-1, "workspace missing, smaller than %zu bytes or not 256-byte aligned", need);
   // (with top-k the few tokens that stay are found faster by one workgroup)
+  const int parts = top_k ? 1 : sample_parts(rows, V, dtype == ELMO_BF16);
+  const size_t need = parts == 1 ? 0 : elmo_sample_bytes(rows, V);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return fail(-1, "workspace missing, smaller than %zu bytes or not 256-byte aligned", need);
   const elmo::SampleArgs a{logits, logits_stride, V, u, temperature, top_p, min_p, top_k, idx_out, prob_out, std::min(50, 62 - bits),
-                           top_k ? 1 : sample_parts(rows, V, dtype == ELMO_BF16), (char*)workspace};
+                           parts, (char*)workspace};
   hipStream_t st = (hipStream_t)hip_stream;
   return dtype == ELMO_BF16 ? launch_sample<uint16_t>(a, rows, st) : launch_sample<float>(a, rows, st);
 }
@@ -303,6 +314,7 @@ int distill_parts(int64_t rows, int64_t V) {
   return (int)((rounds + per - 1) / per);
 }
 template <class T> int launch_distill(const elmo::DistillArgs& a, hipStream_t st) {
+  ELMO_TRY(check_grid("elmo_distill", a.rows * a.parts, elmo::kDistillThreads));
   const unsigned grid = (unsigned)(a.rows * a.parts);
   if (a.parts == 1) {
     elmo::k_distill<T, elmo::DISTILL_WHOLE><<<grid, elmo::kDistillThreads, 0, st>>>(a);

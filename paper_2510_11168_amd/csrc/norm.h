@@ -128,7 +128,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm(NormArgs a) {
     const bool bad = !(ms < __builtin_inff()) || m == __builtin_inf();
     const bool live = m > 0.0 && !bad;                    // a row of zeros: zeros with scale 0
     const double inv = 1.0 / m * MOST;                    // the order of these roundings decides exact ties
-    if (in_row == 0 && lane == 0) a.scale[row] = bad ? __builtin_nanf("") : (float)(m * (double)rstd / MOST);
+    if (in_row == 0 && lane == 0) a.scale[row] = bad ? __builtin_nanf("") : live ? (float)(m * (double)rstd / MOST) : 0.0f;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c = c0 + s * STEP;

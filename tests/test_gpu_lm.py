@@ -117,6 +117,8 @@ def test_norm_rows_that_hold_infinities_and_nan(b):
     b.elmo_rms_norm(x, q, None, 1e-6, scale_out=scale)
     assert bool(torch.isnan(scale[1:5]).all()) and not q[1:5].any()
     assert bool((q[[0, 5]] == 127).all()) and bool(torch.isfinite(scale[[0, 5]]).all())
+    b.elmo_rms_norm(torch.zeros_like(x), q, None, 0.0, scale_out=scale)
+    assert not q.any() and not scale.any(), "zeros have scale 0 without eps too"
     w = torch.ones(260, device=DEV)
     w[7] = float("nan")
     b.elmo_rms_norm(x, q, w, 1e-6, scale_out=scale)
@@ -184,6 +186,14 @@ def test_int8_matmul(b, M, N, K, out):
         # sum to FP32, two products, the bias's addition
         close(y, want, 3.01 * E * plain + (HALF[out] + 1.01 * E) * np.abs(want) + 1e-38, f"out, pad {pad}")
         assert between_rows(y) is None or bool((between_rows(y).float() == 72).all())
+
+
+@pytest.mark.parametrize("M,N", [(3, 40), (40, 70), (200, 300)])
+def test_int8_sums_of_nothing(b, M, N):
+    bias, y = torch.randn(N, generator=gen(1)).to(DEV), torch.full((M, N), 9.0, device=DEV)
+    none = lambda r: torch.empty((r, 0), dtype=torch.int8, device=DEV)  # noqa: E731
+    b.elmo_int8_matmul(none(M), torch.ones(M, device=DEV), none(N), torch.ones(N, device=DEV), y, bias=bias)
+    assert torch.equal(y, bias.expand(M, N))
 
 
 def test_int8_offsets_beyond_32_bits(b):

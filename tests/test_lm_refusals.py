@@ -118,6 +118,8 @@ NAN = float("nan")
     (_sample, -1, dict(i=None)), (_sample, -1, dict(zs=63)), (_sample, -1, dict(k=P + 2)), (_sample, -1, dict(z=P + 1)),
     (_distill, -2, dict(dt=1)), (_distill, -2, dict(tt=3)), (_distill, -1, dict(K=0)), (_distill, -1, dict(K=1025)), (_distill, -1, dict(T=0.0)),
     (_distill, -1, dict(T=NAN)), (_distill, -1, dict(T=-1.0)), (_distill, -1, dict(T=1e9)), (_distill, -1, dict(V=0)), (_distill, -1, dict(loss=None)),
+    (_norm, -1, dict(rows=1 << 27)), (_norm, -1, dict(rows=1 << 25, d=2048, xs=2048, ys=2048)), (_sample, -1, dict(rows=1 << 23)),
+    (_distill, -1, dict(rows=1 << 24)), (_int8, -1, dict(M=1 << 30, N=1 << 30, os=1 << 30)),
     (_distill, -1, dict(g=P, gs=5)), (_distill, -1, dict(t=P + 2)), (_distill, -1, dict(i=None)),
 ])
 def test_arguments_that_the_library_refuses(b, call, code, kw):
