@@ -3,7 +3,8 @@
 //   loss = v T^2 sum_j q_j (log q_j - log p_{i_j}),   dloss / dz_i = v T (p_i - sum_{j : i_j = i} q_j),   v = the row's weight.
 //
 // exp is taken as exp2(z c - m c) with c = log2(e) / T: c and m c are rounded once and enter every term of a row alike, so that what m c lost
-// cancels; the sums over V are FP32, the loss's own terms (K of them) FP64.  A token at -infinity has p = 0; a row of weight 0 is not read.
+// cancels; the exponentials are FP32 and summed in octets, the octets' sums and the loss's own terms (K of them) FP64: a loss is a small difference
+// where student and teacher agree.  A token at -infinity has p = 0; a row of weight 0 is not read.
 #pragma once
 #include "rows.h"
 
@@ -30,7 +31,7 @@ struct DistillArgs {
 
 // (maximum, sum of exp2(z c - shift(m, c))) of a part of a row.  A part without a finite logit has m = -infinity and no sum.  Parts are
 // joined by the difference of their rounded shifts, those that their sums were taken with.
-struct MaxSum { float m, s; };
+struct MaxSum { double s; float m; };
 __device__ inline float shift(float m, float c) { return m == -__builtin_inff() ? 0.0f : m * c; }
 __device__ inline float rescale(float m, float c, float mc) { return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m * c - mc); }
 
@@ -61,8 +62,8 @@ enum : int { DISTILL_WHOLE = 0, DISTILL_SUMS = 1, DISTILL_GRADIENT = 2 };
 template <class T, int MODE>
 __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   constexpr int NT = kDistillThreads, NW = NT / 64, PER = kDistillMaxK / NT;
-  __shared__ float s_m[NW], s_s[NW], s_t[NW], s_q[kDistillMaxK], s_z[kDistillMaxK];
-  __shared__ double s_d[NW], s_l[NW], s_x[kDistillMaxK], s_e[kDistillMaxK];
+  __shared__ float s_m[NW], s_t[NW], s_q[kDistillMaxK], s_z[kDistillMaxK];
+  __shared__ double s_s[NW], s_d[NW], s_l[NW], s_x[kDistillMaxK], s_e[kDistillMaxK];
   __shared__ int s_i[kDistillMaxK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = MODE == DISTILL_WHOLE ? blockIdx.x : blockIdx.x / a.parts;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   }
   // ---- student: maximum and sum in one pass
   const float last = tid < tail ? load_one(z, rest + tid) : -__builtin_inff();
-  MaxSum ms = {-__builtin_inff(), 0.0f};
+  MaxSum ms = {0.0, -__builtin_inff()};
   if constexpr (MODE != DISTILL_GRADIENT) {
     if (tid < tail) {
       if (last == last) ms.m = last;                     // (a NaN is in the sum)
@@ -120,18 +121,18 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
     for (int64_t o = r.lo + tid; o < r.hi; o += NT) {
       const Octet<T> oc = load_octet(z + o * 8, 8);
       const float top = octet_max(oc);
-      if (top > ms.m) ms = {top, ms.s * rescale(ms.m, a.c, shift(top, a.c))};
-      ms.s += octet_sum(oc, a.c, shift(ms.m, a.c));
+      if (top > ms.m) ms = {ms.s * (double)rescale(ms.m, a.c, shift(top, a.c)), top};
+      ms.s += (double)octet_sum(oc, a.c, shift(ms.m, a.c));
     }
     const float top = wave_max(ms.m);
-    ms = {top, wave_sum(ms.s * rescale(ms.m, a.c, shift(top, a.c)))};
+    ms = {wave_sum64(ms.s * (double)rescale(ms.m, a.c, shift(top, a.c))), top};
     if (lane == 0) {
       s_m[wave] = ms.m;
       s_s[wave] = ms.s;
     }
     __syncthreads();
     ms.m = slots_reduce<NW>(s_m, lane, [](float p, float q) { return fmaxf(p, q); });
-    ms.s = wave_reduce<NW>(s_s[lane & (NW - 1)] * rescale(s_m[lane & (NW - 1)], a.c, shift(ms.m, a.c)), [](float p, float q) { return p + q; });
+    ms.s = wave_reduce<NW>(s_s[lane & (NW - 1)] * (double)rescale(s_m[lane & (NW - 1)], a.c, shift(ms.m, a.c)), [](double p, double q) { return p + q; });
     if (MODE == DISTILL_SUMS) {
       if (tid == 0) partials[part] = ms;
       return;
@@ -139,11 +140,11 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   } else {
     const MaxSum mine = lane < a.parts ? partials[lane] : ms;    // (at most 64 parts)
     ms.m = wave_max(mine.m);
-    ms.s = wave_sum(mine.s * rescale(mine.m, a.c, shift(ms.m, a.c)));
+    ms.s = wave_sum64(mine.s * (double)rescale(mine.m, a.c, shift(ms.m, a.c)));
   }
   const float mc = shift(ms.m, a.c);
   // ---- gradient: p everywhere
-  const float vT = v * a.T, inv = ms.s == 0.0f ? 0.0f : vT / ms.s;
+  const float vT = v * a.T, inv = ms.s == 0.0 ? 0.0f : vT / (float)ms.s;
   const auto p_of = [&](float f) { return __builtin_amdgcn_exp2f(__builtin_fmaf(f, a.c, -mc)) * inv; };
   if (g) {
     if (tid < tail) store_one(g, rest + tid, p_of(last));
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   if (lane == 0) s_d[wave] = sum;
   __syncthreads();
   sum = slots_reduce<NW>(s_d, lane, [](double p, double q) { return p + q; });
-  const double logsum = log_series(sum), lognorm = log_series((double)ms.s);
+  const double logsum = log_series(sum), lognorm = log_series(ms.s);
   double loss = 0.0;
 #pragma unroll 1
   for (int j = tid; j < a.K; j += NT) {

@@ -151,6 +151,9 @@ template <int NW, class T, class Op> __device__ inline T slots_reduce(const T* s
 __device__ inline float wave_sum(float v) {
   return wave_reduce(v, [](float a, float b) { return a + b; });
 }
+__device__ inline double wave_sum64(double v) {
+  return wave_reduce(v, [](double a, double b) { return a + b; });
+}
 // max of FP32 values without NaN, by their order
 __device__ inline float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
