@@ -54,8 +54,8 @@ __device__ inline Range part_of(int64_t octets, int part, int parts) {
 }
 
 // WHOLE: a row a workgroup.  It is read twice -- 256 rows of a large vocabulary that are worked on at a time fit the memory-side cache, from
-// which the second reading comes -- and the gradient goes past the caches.  4096 x 131072 BF16: 557 us, 3.9 TB/s of what has to move (a copy:
-// 4.8); rows held in registers, with the next one's loads under way as the gradient is written: 559 to 600.
+// which the second reading comes -- and the gradient goes past the caches.  4096 x 131072 BF16: 514 to 540 us, 4.0 TB/s of what has to move
+// (a copy: 4.8); rows held in registers, with the next one's loads under way as the gradient is written: 559 to 652.
 // SUMS, GRADIENT: few rows, in `parts` workgroups each: the parts' maxima and sums with the teacher's tokens' logits, then the gradient with them.  (The
 // second launch takes no logit that another part may already have overwritten.)  One row of 131072: see the launch.
 enum : int { DISTILL_WHOLE = 0, DISTILL_SUMS = 1, DISTILL_GRADIENT = 2 };
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   constexpr int NT = kDistillThreads, NW = NT / 64, PER = kDistillMaxK / NT;
   __shared__ float s_m[NW], s_t[NW], s_q[kDistillMaxK], s_z[kDistillMaxK];
   __shared__ double s_s[NW], s_d[NW], s_l[NW], s_x[kDistillMaxK], s_e[kDistillMaxK];
-  __shared__ int s_i[kDistillMaxK];
+  __shared__ int s_i[kDistillMaxK], s_seen[2 * kDistillMaxK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = MODE == DISTILL_WHOLE ? blockIdx.x : blockIdx.x / a.parts;
   const int part = MODE == DISTILL_WHOLE ? 0 : (int)(blockIdx.x % a.parts);
@@ -77,29 +77,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   MaxSum* partials = (MaxSum*)a.ws + row * a.parts;
   float* token_z = (float*)((MaxSum*)a.ws + a.rows * a.parts) + row * kDistillMaxK;
   const float v = a.v ? a.v[row] : 1.0f;
-  // ---- the teacher's tokens and its largest logit
-  float m = -__builtin_inff();
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int j = i * NT + tid;
-    if (j < a.K) {
-      int at = a.ti[row * a.K + j];
-      float t = a.t32 ? ((const float*)a.tz)[row * a.K + j] : bf16_decode(((const uint16_t*)a.tz)[row * a.K + j]);
-      if (!(t == t)) t = __builtin_inff();               // a NaN teacher makes the row NaN, by inf - inf
-      if (at < 0 || at >= a.V) { at = -1; t = -__builtin_inff(); }
-      s_i[j] = at;
-      s_x[j] = (double)t;
-      if (MODE != DISTILL_GRADIENT) s_z[j] = at >= 0 && v != 0.0f ? load_one(z, at) : 0.0f;
-      else s_z[j] = v != 0.0f ? token_z[j] : 0.0f;
-      if (MODE == DISTILL_SUMS && part == 0 && v != 0.0f) token_z[j] = s_z[j];
-      m = fmaxf(m, t);
-    }
-  }
-  m = wave_max(m);
-  if (lane == 0) s_t[wave] = m;
-  __syncthreads();
-  m = slots_reduce<NW>(s_t, lane, [](float p, float q) { return fmaxf(p, q); });
-  if (m == -__builtin_inff() || v == 0.0f) {             // no teacher, or a row that does not count
+  const auto zeros = [&]() {                             // of a row without a teacher, or one that does not count
     if (MODE == DISTILL_SUMS) return;
     if (g) {
       const float zero[8] = {};
@@ -107,7 +85,27 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
       if (tid < tail) store_one(g, rest + tid, 0.0f);
     }
     if (tid == 0 && part == 0) a.loss[row] = 0.0f;
-    return;
+  };
+  if (v == 0.0f) return zeros();
+  // a table of the teacher's tokens, at least twice as large as they are many: which of them come more than once
+  int bits = 6;
+  while ((1 << bits) < 2 * a.K) ++bits;
+  const auto first_slot = [&](int token) { return (int)(((uint32_t)token * 2654435761u) >> (32 - bits)); };
+  constexpr int kTwice = (int)0x80000000;
+  if (MODE != DISTILL_SUMS)
+    for (int i = tid; i < 1 << bits; i += NT) s_seen[i] = -1;
+  // ---- the teacher's tokens go out first, their logits of the student behind its row: two trips to memory that nothing waits for
+  int at[PER];
+  float t[PER], zi[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * NT + tid;
+    at[i] = -1;
+    t[i] = -__builtin_inff();
+    if (j < a.K) {
+      at[i] = a.ti[row * a.K + j];
+      t[i] = a.t32 ? ((const float*)a.tz)[row * a.K + j] : bf16_decode(((const uint16_t*)a.tz)[row * a.K + j]);
+    }
   }
   // ---- student: maximum and sum in one pass
   const float last = tid < tail ? load_one(z, rest + tid) : -__builtin_inff();
@@ -124,13 +122,53 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
       if (top > ms.m) ms = {ms.s * (double)rescale(ms.m, a.c, shift(top, a.c)), top};
       ms.s += (double)octet_sum(oc, a.c, shift(ms.m, a.c));
     }
+  }
+  float m = -__builtin_inff();                           // the teacher's largest logit
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * NT + tid;
+    if (!(t[i] == t[i])) t[i] = __builtin_inff();        // a NaN teacher makes the row NaN, by inf - inf
+    if (at[i] < 0 || at[i] >= a.V) { at[i] = -1; t[i] = -__builtin_inff(); }
+    zi[i] = 0.0f;
+    if (MODE == DISTILL_GRADIENT) zi[i] = j < a.K ? token_z[j] : 0.0f;
+    else if (at[i] >= 0) zi[i] = load_one(z, at[i]);
+    if (MODE == DISTILL_SUMS && part == 0 && j < a.K) token_z[j] = zi[i];
+    m = fmaxf(m, t[i]);
+  }
+  if constexpr (MODE != DISTILL_GRADIENT) {
     const float top = wave_max(ms.m);
     ms = {wave_sum64(ms.s * (double)rescale(ms.m, a.c, shift(top, a.c))), top};
     if (lane == 0) {
       s_m[wave] = ms.m;
       s_s[wave] = ms.s;
     }
-    __syncthreads();
+  }
+  m = wave_max(m);
+  if (lane == 0) s_t[wave] = m;
+  if (MODE != DISTILL_SUMS) {
+    __syncthreads();                                     // (the table is empty)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = i * NT + tid;
+      if (j < a.K) {
+        s_i[j] = at[i];
+        s_x[j] = (double)t[i];
+        s_z[j] = zi[i];
+      }
+      if (at[i] >= 0)
+        for (int h = first_slot(at[i]);; h = (h + 1) & ((1 << bits) - 1)) {     // (ends: half of the table stays empty)
+          const int there = atomicCAS(&s_seen[h], -1, at[i]);
+          if (there == -1) break;
+          if ((there & ~kTwice) == at[i]) {
+            atomicOr(&s_seen[h], kTwice);
+            break;
+          }
+        }
+    }
+  }
+  __syncthreads();
+  m = slots_reduce<NW>(s_t, lane, [](float p, float q) { return fmaxf(p, q); });
+  if constexpr (MODE != DISTILL_GRADIENT) {
     ms.m = slots_reduce<NW>(s_m, lane, [](float p, float q) { return fmaxf(p, q); });
     ms.s = wave_reduce<NW>(s_s[lane & (NW - 1)] * (double)rescale(s_m[lane & (NW - 1)], a.c, shift(ms.m, a.c)), [](double p, double q) { return p + q; });
     if (MODE == DISTILL_SUMS) {
@@ -142,6 +180,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
     ms.m = wave_max(mine.m);
     ms.s = wave_sum64(mine.s * (double)rescale(mine.m, a.c, shift(ms.m, a.c)));
   }
+  if (m == -__builtin_inff()) return zeros();
   const float mc = shift(ms.m, a.c);
   // ---- gradient: p everywhere
   const float vT = v * a.T, inv = ms.s == 0.0 ? 0.0f : vT / (float)ms.s;
@@ -185,21 +224,27 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   loss = slots_reduce<NW>(s_l, lane, [](double p, double q) { return p + q; });
   if (tid == 0 && part == 0) a.loss[row] = (float)(loss * (double)a.T * (double)a.T * (double)v);
   if (!g) return;
-  // ---- the teacher's tokens once more (of equal ones the first, for all), each by the part that wrote it
+  // ---- the teacher's tokens once more, each by the part that wrote it; of equal ones the first, for all
   const int64_t from = r.lo * 8, to = r.hi * 8 + tail;
 #pragma unroll 1
   for (int k = tid; k < a.K; k += NT) {
-    const int at = s_i[k];
-    if (at < 0 || at < from || at >= to) continue;
-    float all = 0.0f;
-    int first = k;
-#pragma unroll 4
-    for (int j = 0; j < a.K; ++j)
-      if (s_i[j] == at) {
-        first = min(first, j);
-        all += s_q[j];
+    const int token = s_i[k];
+    if (token < 0 || token < from || token >= to) continue;
+    int h = first_slot(token);
+    while ((s_seen[h] & ~kTwice) != token) h = (h + 1) & ((1 << bits) - 1);
+    float all = s_q[k];
+    if (s_seen[h] < 0) {
+      int first = k;
+      all = 0.0f;
+#pragma unroll 8
+      for (int j = 0; j < a.K; ++j) {                    // (without branches: the reads of several tokens are under way together)
+        const bool same = s_i[j] == token;
+        first = same ? min(first, j) : first;
+        all += same ? s_q[j] : 0.0f;
       }
-    if (first == k) store_one(g, at, p_of(s_z[k]) - vT * all);
+      if (first != k) continue;
+    }
+    store_one(g, token, p_of(s_z[k]) - vT * all);
   }
 }
 

@@ -247,8 +247,8 @@ constexpr int64_t kMostV = ((int64_t)1 << 31) - 1;
 }
 
 namespace {
-// Workgroups of a row without top-k: one where the rows fill the chip or are short.  Rows of 131072, top-p: 128 in FP32 67 us split (121 whole), in BF16,
-// which one workgroup takes by codes, 68 split and 58 whole; 1 row 28 and 120.  One row of 8192 FP32: 25.6 split, 18.9 whole.
+// Workgroups of a row without top-k: one where the rows fill the chip or are short.  Rows of 131072, top-p: 128 in FP32 72 us split (120 whole), 1 row 27
+// (109); in BF16, which one workgroup takes by codes, 128 rows 68 (58), 64 rows 51 (56), 1 row 28 (56).  One row of 16384 FP32: 25.8 (25.0).
 constexpr int64_t kSampleSplitRows = 128, kSampleSplitV = 16384;
 int sample_parts(int64_t rows, int64_t V, bool bf16) {
   if (rows > (bf16 ? kSampleSplitRows / 2 : kSampleSplitRows) || V < kSampleSplitV) return 1;
