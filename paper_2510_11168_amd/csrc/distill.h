@@ -2,9 +2,9 @@
 // teacher's tokens:
 //   loss = v T^2 sum_j q_j (log q_j - log p_{i_j}),   dloss / dz_i = v T (p_i - sum_{j : i_j = i} q_j),   v = the row's weight.
 //
-// exp is taken as exp2(z c - m c) with c = log2(e) / T: c and m c are rounded once and enter every term of a row alike, so that what m c lost
-// cancels; the exponentials are FP32 and summed in octets, the octets' sums and the loss's own terms (K of them) FP64: a loss is a small difference
-// where student and teacher agree.  A token at -infinity has p = 0; a row of weight 0 is not read.
+// exp((z - m) / T) is taken as exp2((z - m) c) with c = log2(e) / T; the difference first, so that rows of the type's lowest value, whose product with c
+// overflows, are rows like others.  The exponentials are FP32 and summed in octets, the octets' sums and the loss's own terms (K of them) FP64: a
+// loss is a small difference where student and teacher agree.  A token at -infinity has p = 0; a row of weight 0 is not read.
 #pragma once
 #include "rows.h"
 
@@ -29,17 +29,17 @@ struct DistillArgs {
   void* ws;                          // of split rows: [rows, parts] MaxSum, [rows, kDistillMaxK] logits of the teacher's tokens
 };
 
-// (maximum, sum of exp2(z c - shift(m, c))) of a part of a row.  A part without a finite logit has m = -infinity and no sum.  Parts are
-// joined by the difference of their rounded shifts, those that their sums were taken with.
+// (maximum, sum of exp2((z - base(m)) c)) of a part of a row.  A part without a finite logit has m = -infinity and no sum.
 struct MaxSum { double s; float m; };
-__device__ inline float shift(float m, float c) { return m == -__builtin_inff() ? 0.0f : m * c; }
-__device__ inline float rescale(float m, float c, float mc) { return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m * c - mc); }
+__device__ inline float base(float m) { return m == -__builtin_inff() ? 0.0f : m; }
+__device__ inline float power(float z, float from, float c) { return __builtin_amdgcn_exp2f((z - from) * c); }
+__device__ inline double rescale(float m, float to, float c) { return m == -__builtin_inff() ? 0.0 : (double)power(m, base(to), c); }
 
-// The exponentials of an octet against shift mc, summed.
-template <class T> __device__ inline float octet_sum(const Octet<T>& o, float c, float mc) {
+// The exponentials of an octet, summed.
+template <class T> __device__ inline float octet_sum(const Octet<T>& o, float from, float c) {
   float e[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(o[i], c, -mc));
+  for (int i = 0; i < 8; ++i) e[i] = power(o[i], from, c);
   return ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 }
 template <class T> __device__ inline float octet_max(const Octet<T>& o) {
@@ -113,14 +113,14 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   if constexpr (MODE != DISTILL_GRADIENT) {
     if (tid < tail) {
       if (last == last) ms.m = last;                     // (a NaN is in the sum)
-      ms.s = __builtin_amdgcn_exp2f(__builtin_fmaf(last, a.c, -shift(ms.m, a.c)));
+      ms.s = power(last, base(ms.m), a.c);
     }
 #pragma unroll 4
     for (int64_t o = r.lo + tid; o < r.hi; o += NT) {
       const Octet<T> oc = load_octet(z + o * 8, 8);
       const float top = octet_max(oc);
-      if (top > ms.m) ms = {ms.s * (double)rescale(ms.m, a.c, shift(top, a.c)), top};
-      ms.s += (double)octet_sum(oc, a.c, shift(ms.m, a.c));
+      if (top > ms.m) ms = {ms.s * rescale(ms.m, top, a.c), top};
+      ms.s += (double)octet_sum(oc, base(ms.m), a.c);
     }
   }
   float m = -__builtin_inff();                           // the teacher's largest logit
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   }
   if constexpr (MODE != DISTILL_GRADIENT) {
     const float top = wave_max(ms.m);
-    ms = {wave_sum64(ms.s * (double)rescale(ms.m, a.c, shift(top, a.c))), top};
+    ms = {wave_sum64(ms.s * rescale(ms.m, top, a.c)), top};
     if (lane == 0) {
       s_m[wave] = ms.m;
       s_s[wave] = ms.s;
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   m = slots_reduce<NW>(s_t, lane, [](float p, float q) { return fmaxf(p, q); });
   if constexpr (MODE != DISTILL_GRADIENT) {
     ms.m = slots_reduce<NW>(s_m, lane, [](float p, float q) { return fmaxf(p, q); });
-    ms.s = wave_reduce<NW>(s_s[lane & (NW - 1)] * (double)rescale(s_m[lane & (NW - 1)], a.c, shift(ms.m, a.c)), [](double p, double q) { return p + q; });
+    ms.s = wave_reduce<NW>(s_s[lane & (NW - 1)] * rescale(s_m[lane & (NW - 1)], ms.m, a.c), [](double p, double q) { return p + q; });
     if (MODE == DISTILL_SUMS) {
       if (tid == 0) partials[part] = ms;
       return;
@@ -178,13 +178,13 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   } else {
     const MaxSum mine = lane < a.parts ? partials[lane] : ms;    // (at most 64 parts)
     ms.m = wave_max(mine.m);
-    ms.s = wave_sum64(mine.s * (double)rescale(mine.m, a.c, shift(ms.m, a.c)));
+    ms.s = wave_sum64(mine.s * rescale(mine.m, ms.m, a.c));
   }
   if (m == -__builtin_inff()) return zeros();
-  const float mc = shift(ms.m, a.c);
+  const float from_z = base(ms.m);
   // ---- gradient: p everywhere
   const float vT = v * a.T, inv = ms.s == 0.0 ? 0.0f : vT / (float)ms.s;
-  const auto p_of = [&](float f) { return __builtin_amdgcn_exp2f(__builtin_fmaf(f, a.c, -mc)) * inv; };
+  const auto p_of = [&](float f) { return power(f, from_z, a.c) * inv; };
   if (g) {
     if (tid < tail) store_one(g, rest + tid, p_of(last));
 #pragma unroll 4
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kDistillThreads) void k_distill(DistillArgs a) {
   for (int j = tid; j < a.K; j += NT) {
     const double q = s_e[j] / sum;
     if (s_i[j] >= 0 && !(q == 0.0))
-      loss += ms.m == -__builtin_inff() ? (double)__builtin_inff() : q * (s_x[j] - logsum - kLn2 * ((double)s_z[j] * (double)a.c - (double)mc) + lognorm);
+      loss += ms.m == -__builtin_inff() ? (double)__builtin_inff() : q * (s_x[j] - logsum - ((double)s_z[j] - (double)from_z) / (double)a.T + lognorm);
     s_q[j] = (float)q;
   }
   loss = wave_reduce(loss, [](double p, double q) { return p + q; });

@@ -32,12 +32,14 @@ template <class O> __device__ inline void store_out(const Int8Args& p, int m, in
 
 // ---------------------------------------------------------------------------------------------
 // The product in tiles of TM x TN outputs (waves of 32 FM x 32 FN) over slabs of 128 bytes of K.
-// ASYNC, for operands whose rows are 16-byte aligned: slabs go to LDS by asynchronous loads, NST stages; as in ring_stream_pp half of the waves issue behind the barrier
-// (all of A and half of B) and half in the middle of the slab, so that one wave of every SIMD multiplies while the other is held by its loads.
+// ASYNC, for operands whose rows are 16-byte aligned: slabs go to LDS by asynchronous loads, NST stages; as in ring_stream_pp half of the waves
+// issue behind the barrier (all of A and half of B) and half in the middle of the slab, so that one wave of every SIMD multiplies while the other is
+// held by its loads.
 // Otherwise a slab goes through registers, its loads in flight while the one before is multiplied, to the other of two stages.
 // v_mfma_i32_32x32x32_i8: lane i holds row i % 32 of an operand, 16 bytes of K from 16 (i / 32) on.
 // Tile row 32 j + l of a wave's columns holds weight row FN l + j: a lane then has FN neighbouring outputs of a row, and a wave stores 32 FN of them next
-// to each other.
+// to each other.  8192 x 14336 x 4096 in tiles of 256 x 256: 404 to 444 us, 2.2 to 2.4 POP/s (the library's product of that size, without scales: 442);
+// bound by the matrix cores, 64 % busy, and their clock, which falls under random values.  Through registers: 574.
 // ---------------------------------------------------------------------------------------------
 template <int FN> struct Interleave {
   __device__ inline int operator()(int r) const { return (r & ~(32 * FN - 1)) + (r & 31) * FN + ((r >> 5) & (FN - 1)); }
@@ -231,8 +233,8 @@ __global__ __launch_bounds__((int8_threads<TM, TN, FM, FN>())) void k_int8_tiles
 }
 
 // ---------------------------------------------------------------------------------------------
-// Few tokens (at most 16 FM): the stream of the weights is the work (1 x 28672 x 8192: 37.6 us, 6.3 TB/s).  A workgroup has 16 weight rows, its eight waves take every eighth 256 bytes of
-// K, and their sums are added in LDS.  Both operands go from memory to registers as v_mfma_i32_16x16x64_i8 takes them (lane i: row
+// Few tokens (at most 16 FM): the stream of the weights is the work (1 x 28672 x 8192: 37.6 us, 6.3 TB/s).  A workgroup has 16 weight rows, its eight
+// waves take every eighth 256 bytes of K, and their sums are added in LDS.  Both operands go from memory to registers as v_mfma_i32_16x16x64_i8 takes them (lane i: row
 // i % 16, 16 bytes from 16 (i / 16) on), four loads of each in flight; rows may begin anywhere.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSkinnyThreads = 512, kSkinnySlab = 256;

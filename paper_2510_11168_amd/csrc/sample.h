@@ -90,7 +90,7 @@ __device__ inline RowSettings settings_of(const SampleArgs& a, int64_t row) {
   const bool greedy = !(t > 0.0f);
   s.t = greedy ? 1.0 : (double)t;
   s.k = greedy ? 1 : k > 0 && k < a.V ? k : a.V;
-  s.p = p < 1.0f ? (double)p : 1.0;            // NaN: off
+  s.p = p < 1.0f ? fmax((double)p, 0.0) : 1.0; // NaN: off
   s.mp = mp > 0.0f ? (mp < 1.0f ? (double)mp : 1.0) : 0.0;
   s.u = u > 0.0f ? (double)u : 0.0;
   return s;

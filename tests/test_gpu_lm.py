@@ -466,6 +466,23 @@ def test_distill_masked_logits_and_odd_teachers(b):
     assert loss[5] == 0 and not grad[5].any()
 
 
+@pytest.mark.parametrize("T", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_distill_rows_masked_with_the_types_lowest_value(b, T, dtype):
+    """The lowest value as a mask: beside other logits p = 0, in a row of nothing else all tokens alike."""
+    low, V = torch.finfo(dtype).min, 1003
+    z = torch.randn((3, V), generator=gen(6)).to(dtype)
+    z[0, ::2], z[1], z[2] = low, low, -low
+    idx, tz = torch.tensor([[1, 3], [0, 7], [0, 7]], dtype=torch.int32), torch.tensor([[0.5, 0.0]] * 3)
+    loss, grad = torch.empty(3, device=DEV), torch.empty((3, V), dtype=dtype, device=DEV)
+    b.elmo_distill(z.to(DEV), idx.to(DEV), tz.to(DEV), loss, grad, temperature=T)
+    want = o.distill(f64(z), idx.numpy(), f64(tz), T)
+    tl, tg = distill_tolerance(z, idx, tz, T, None, dtype, want)
+    close(loss, want[0], tl, "loss")
+    close(grad, want[1], tg, "gradient")
+    assert not grad[0, ::2].any()
+
+
 @pytest.mark.parametrize("rows,V", [(3, 40), (2, 3000)])
 def test_distill_gradient_is_that_of_its_loss(b, rows, V):
     """Central differences of the FP32 loss along random directions."""
