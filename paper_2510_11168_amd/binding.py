@@ -260,10 +260,10 @@ def _vector(name, t, types, n):
     return t.data_ptr(), code
 
 
-def _needed(**tensors):
-    for name, t in tensors.items():
+def _needed(names, *tensors):
+    for t in tensors:
         if t is None:
-            raise ElmoError(-1, f"{name} is missing")
+            raise ElmoError(-1, f"{names}: all of them are needed")
 
 
 def _call(fn, args, tensors, stream, workspace=None, bytes_needed=None):
@@ -298,7 +298,7 @@ def _call(fn, args, tensors, stream, workspace=None, bytes_needed=None):
 
 def elmo_rms_norm(x, y, weight=None, eps=1e-6, *, residual=None, sum_out=None, scale_out=None, stream=None) -> None:
     """y <- weight * h / sqrt(mean(h^2) + eps), h = x + residual; sum_out <- h; 8-bit y (int8, E4M3): scale_out <- the rows' scales."""
-    _needed(x=x, y=y)
+    _needed("x, y", x, y)
     xp, xs, dtype = _matrix("x", x, _REAL)
     rows, d = x.shape
     real = _SAME[dtype]
@@ -317,7 +317,7 @@ def elmo_rms_norm_backward_bytes(rows, d) -> int:
 
 def elmo_rms_norm_backward(dy, h, dh, weight=None, eps=1e-6, *, dsum=None, dweight=None, workspace=None, stream=None) -> None:
     """dh <- gradient of h (plus dsum), dweight <- gradient of the weight."""
-    _needed(dy=dy, h=h, dh=dh)
+    _needed("dy, h, dh", dy, h, dh)
     yp, ys, dtype = _matrix("dy", dy, _REAL)
     rows, d = dy.shape
     real = _SAME[dtype]
@@ -332,7 +332,7 @@ def elmo_rms_norm_backward(dy, h, dh, weight=None, eps=1e-6, *, dsum=None, dweig
 
 def elmo_int8_matmul(a, a_scale, b, b_scale, out, bias=None, *, stream=None) -> None:
     """out[m, n] <- (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]."""
-    _needed(a=a, a_scale=a_scale, b=b, b_scale=b_scale, out=out)
+    _needed("a, a_scale, b, b_scale, out", a, a_scale, b, b_scale, out)
     ap, as_, _ = _matrix("a", a, _ONLY_INT8)
     M, K = a.shape
     bp, bs, _ = _matrix("b", b, _ONLY_INT8, None, K)
@@ -350,7 +350,7 @@ def elmo_sample_bytes(rows, V) -> int:
 
 def elmo_sample(logits, u, idx_out, *, temperature=None, top_k=None, top_p=None, min_p=None, prob_out=None, workspace=None, stream=None) -> None:
     """idx_out <- one token a row by temperature, top-k, top-p and min-p from the random numbers u; prob_out <- its probability among the kept."""
-    _needed(logits=logits, u=u, idx_out=idx_out)
+    _needed("logits, u, idx_out", logits, u, idx_out)
     zp, zs, dtype = _matrix("logits", logits, _REAL)
     rows, V = logits.shape
     up, _ = _vector("u", u, _ONLY_FP32, rows)
@@ -371,7 +371,7 @@ def elmo_distill_bytes(rows, V) -> int:
 def elmo_distill(logits, teacher_idx, teacher_logits, loss_out, grad_out=None, *, temperature=1.0, row_weight=None, workspace=None,
                  stream=None) -> None:
     """loss_out <- row_weight T^2 KL(teacher's top tokens || student) for each row, grad_out <- its gradient by the logits."""
-    _needed(logits=logits, teacher_idx=teacher_idx, teacher_logits=teacher_logits, loss_out=loss_out)
+    _needed("logits, teacher_idx, teacher_logits, loss_out", logits, teacher_idx, teacher_logits, loss_out)
     zp, zs, dtype = _matrix("logits", logits, _REAL)
     rows, V = logits.shape
     tp, ts, _ = _matrix("teacher_idx", teacher_idx, _ONLY_INT32, rows)

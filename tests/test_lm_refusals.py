@@ -60,6 +60,15 @@ def test_tensors_that_do_not_fit_together(b):
     refused(b, -1, b.elmo_distill, f(2, 8), i32(2, 3), f(2, 3), f(2), f(2, 7))
 
 
+def test_every_needed_tensor_is_named(b):
+    calls = [(b.elmo_rms_norm, [f(2, 8), f(2, 8)]), (b.elmo_rms_norm_backward, [f(2, 8), f(2, 8), f(2, 8)]),
+             (b.elmo_int8_matmul, [i8(2, 8), f(2), i8(3, 8), f(3), f(2, 3)]), (b.elmo_sample, [f(2, 8), f(2), i32(2)]),
+             (b.elmo_distill, [f(2, 8), i32(2, 3), f(2, 3), f(2)])]
+    for fn, tensors in calls:
+        for i in range(len(tensors)):
+            assert "needed" in refused(b, -1, fn, *tensors[:i], None, *tensors[i + 1:])
+
+
 def test_host_tensors_are_refused(b):
     assert "GPU" in refused(b, -1, b.elmo_rms_norm, f(2, 8), f(2, 8))
     assert "GPU" in refused(b, -1, b.elmo_rms_norm_backward, f(2, 8), f(2, 8), f(2, 8))
