@@ -178,9 +178,12 @@ constexpr size_t kSampleRowBytes = (sizeof(SampleWs) + 255) / 256 * 256;
 // logit].  Slots in falling order.  (Logits nearer to zero than that, should there be any, send a row the other way.)
 constexpr int kCodeOctaves = 21, kCodeHalf = kCodeOctaves * 128, kCodes = 2 * kCodeHalf, kCodesEach = (kCodes + kSampleThreads - 1) / kSampleThreads;
 struct SampleCodes {
-  uint64_t weight[kCodesEach * kSampleThreads];
+  uint64_t weight[kCodesEach * kSampleThreads];              // (behind the slots: no weight)
   uint32_t count[kCodesEach * kSampleThreads];
 };
+static_assert(kCodes < kCodesEach * kSampleThreads, "an entry of no weight");
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
 // One row in the hands of a workgroup.  Everything inlined into the kernels: called, its state would lie in scratch memory and LDS would be reached through flat addresses.
 template <class T> struct Sampler {
@@ -515,10 +518,35 @@ template <class T> struct Sampler {
   }
 
   // ---- BF16, by codes.  False: not this row.
-  __device__ __forceinline__ int slot(uint32_t code, int base) const {    // negative or beyond kCodes: none
-    const int i = (int)(code & 0x7FFF) - base;
-    const int s = code & 0x8000 ? kCodeHalf + i : kCodeHalf - 1 - i;
-    return (uint32_t)i < (uint32_t)kCodeHalf ? s : -1;
+  static constexpr int kNoEnd = 1 << 16;       // beyond what slots_of gives
+  static constexpr int kFlight = 4;            // octets of a thread on their way at a time
+  __device__ __forceinline__ Octet<uint16_t> load_codes(int64_t o) const {            // (beyond the row: -infinity)
+    constexpr uint32_t none = 0xFF80FF80u;
+    if (o >= octets) return {{none, none, none, none}};
+    return load_octet((const uint16_t*)z + o * 8, a.V - o * 8, 0xFF80u);
+  }
+  static __device__ __forceinline__ bool has_small(const Octet<uint16_t>& oc, int base) {
+    const auto sizes = [&](int i) { return __builtin_bit_cast(u16x2, oc.v[i] & 0x7FFF7FFFu); };
+    const u16x2 m = __builtin_elementwise_min(__builtin_elementwise_min(sizes(0), sizes(1)), __builtin_elementwise_min(sizes(2), sizes(3)));
+    return min(m[0], m[1]) < base;
+  }
+  // Adds an octet's logits nearer to zero than the slots go, of at least a weight.
+  __device__ __forceinline__ void next_to_zero(int64_t o, int base, uint64_t from, uint64_t& mass, uint64_t& tokens) const {
+#pragma unroll 1
+    for (int64_t i = o * 8; i < min(a.V, o * 8 + 8); ++i) {
+      const float f = load_one((const uint16_t*)z, i);
+      if ((int)(f2u(f) >> 16 & 0x7FFF) >= base) continue;
+      const uint64_t w = weigh(f);
+      mass += w >= from ? w : 0;
+      tokens += w >= from;
+    }
+  }
+  // The slots of two codes at a time, in packed 16-bit arithmetic (three instructions a code).  kCodes and more: none.
+  static __device__ __forceinline__ u16x2 slots_of(uint32_t codes, int base) {
+    const u16x2 from = {(uint16_t)base, (uint16_t)base}, half = {kCodeHalf, kCodeHalf};
+    const u16x2 i = __builtin_elementwise_min(__builtin_bit_cast(u16x2, codes & 0x7FFF7FFFu) - from, half);     // (below base: 2^15 and more)
+    const uint32_t sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, codes) >> 15);
+    return __builtin_bit_cast(u16x2, ~(__builtin_bit_cast(uint32_t, i) ^ sign)) + half;
   }
   __device__ __forceinline__ bool by_code(SampleCodes* c) {
     if (infinite) return false;
@@ -536,29 +564,25 @@ template <class T> struct Sampler {
       c->count[s] = 0;
     }
     __syncthreads();
-    int end = kCodes;                                    // slots before this one are kept, of its own tokens the first `ties`
+    int end = kNoEnd;                                    // slots before this one are kept, of its own tokens the first `ties`
     uint64_t ties = 0;
     if (rs.k < a.V || rs.p < 1.0) {
       uint64_t zero_mass = 0, zero_tokens = 0;           // of the logits nearer to zero
-#pragma unroll 4
-      for (int64_t o = tid; o < octets; o += NT) {
-        const Octet<uint16_t> oc = load_octet((const uint16_t*)z + o * 8, a.V - o * 8, 0xFF80u);
-        bool small = false;
+      for (int64_t o0 = tid; o0 < octets; o0 += kFlight * NT) {
+        Octet<uint16_t> oc[kFlight];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t code = (i & 1) ? oc.v[i >> 1] >> 16 : oc.v[i >> 1] & 0xFFFFu;
-          const int s = slot(code, base);
-          small |= (int)(code & 0x7FFF) < base;
-          if (s >= 0) atomicAdd(&c->count[s], 1u);
-        }
-        if (small) {
+        for (int q = 0; q < kFlight; ++q) oc[q] = load_codes(o0 + q * NT);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if ((int)(f2u(oc[i]) >> 16 & 0x7FFF) < base) {
-              const uint64_t w = weigh(oc[i]);
-              zero_mass += w;
-              zero_tokens += w != 0;
-            }
+        for (int q = 0; q < kFlight; ++q) {
+          u16x2 most = {0, 0};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const u16x2 s = slots_of(oc[q].v[i], base);
+            most = __builtin_elementwise_max(most, s);
+            if (s[0] < kCodes) atomicAdd(&c->count[s[0]], 1u);
+            if (s[1] < kCodes) atomicAdd(&c->count[s[1]], 1u);
+          }
+          if (max(most[0], most[1]) >= kCodes && has_small(oc[q], base)) next_to_zero(o0 + q * NT, base, 1, zero_mass, zero_tokens);
         }
       }
       block_scan(zero_mass, l.sum, wave, lane, zero_mass);
@@ -582,7 +606,7 @@ template <class T> struct Sampler {
       const auto find = [&](bool by_mass, uint64_t want) {
         uint64_t at_n = before, at_m = mass_before;
         __syncthreads();
-        if (tid == 0) l.found[0] = kCodes;               // (stays so if the filter ends next to zero)
+        if (tid == 0) l.found[0] = kNoEnd;               // (stays so if the filter ends next to zero)
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kCodesEach; ++i) {
@@ -603,66 +627,68 @@ template <class T> struct Sampler {
       };
       if ((uint64_t)rs.k < live) {
         total = find(false, (uint64_t)rs.k);
-        if (end == kCodes) return false;
+        if (end == kNoEnd) return false;
       }
       if (rs.p < 1.0) {
         find(true, share_of(rs.p, total));
-        if (end == kCodes) return false;
+        if (end == kNoEnd) return false;
       }
     }
     const bool keep_zero = end >= kCodeHalf;
     // what is not kept has no weight from here on; the last code's tokens count apart
-    uint64_t we = end < kCodes ? c->weight[end] : 0;
+    uint64_t we = end != kNoEnd ? c->weight[end] : 0;
     if (we < least) we = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kCodesEach; ++i)
       if (s0 + i >= end || c->weight[s0 + i] < least) c->weight[s0 + i] = 0;
     __syncthreads();
-    // an octet's weights without the last code's, and which of it are that
-    const auto octet = [&](int64_t o, uint64_t (&w)[8], uint32_t& mask) {
+    // an octet's weights without the last code's, and which of it are that.  (What is not kept reads one entry, all lanes the same: no bank conflicts.)
+    const uint16_t none = (uint16_t)min(end, kCodes);
+    const auto octet = [&](const Octet<uint16_t>& oc, uint64_t (&w)[8], uint32_t& mask, bool& others) {
       uint64_t sum = 0;
       mask = 0;
-      bool small = false;
-      if (o < octets) {
-        const Octet<uint16_t> oc = load_octet((const uint16_t*)z + o * 8, a.V - o * 8, 0xFF80u);
+      u16x2 most = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t code = (i & 1) ? oc.v[i >> 1] >> 16 : oc.v[i >> 1] & 0xFFFFu;
-          const int s = slot(code, base);
-          small |= (int)(code & 0x7FFF) < base;
-          w[i] = s >= 0 ? c->weight[s] : 0;
-          mask |= s == end ? 1u << i : 0;
-          sum += w[i];
-        }
-        if (small && keep_zero) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if ((int)(f2u(oc[i]) >> 16 & 0x7FFF) < base) {
-              w[i] = weigh(oc[i]);
-              if (w[i] < least) w[i] = 0;
-              sum += w[i];
-            }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 0;
+      for (int i = 0; i < 4; ++i) {
+        const u16x2 s = slots_of(oc.v[i], base), in = __builtin_elementwise_min(s, (u16x2){none, none});
+        most = __builtin_elementwise_max(most, s);
+        w[2 * i] = c->weight[in[0]];
+        w[2 * i + 1] = c->weight[in[1]];
+        mask |= (s[0] == end ? 1u << (2 * i) : 0) | (s[1] == end ? 2u << (2 * i) : 0);
+        sum += w[2 * i] + w[2 * i + 1];
       }
+      others = keep_zero && max(most[0], most[1]) >= kCodes && has_small(oc, base);
       return sum;
     };
-    for (int s = wave; s < segments; s += kSampleWaves) {
-      uint64_t sum = 0, w[8];
-      uint32_t count = 0, mask;
+    for (int s = wave; s < segments; s += kFlight * kSampleWaves) {      // (beyond the last segment: no octets)
+      uint64_t sum[kFlight], w[8], unused = 0;
+      uint32_t count[kFlight], mask;
+      bool others;
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q) sum[q] = count[q] = 0;
       for (int64_t i = 0; i < per; ++i) {
-        sum += octet((s * per + i) * 64 + lane, w, mask);
-        count += __popc(mask);
+        Octet<uint16_t> oc[kFlight];
+#pragma unroll
+        for (int q = 0; q < kFlight; ++q) oc[q] = load_codes(((s + q * kSampleWaves) * per + i) * 64 + lane);
+#pragma unroll
+        for (int q = 0; q < kFlight; ++q) {
+          sum[q] += octet(oc[q], w, mask, others);
+          count[q] += __popc(mask);
+          if (others) next_to_zero(((s + q * kSampleWaves) * per + i) * 64 + lane, base, least, sum[q], unused);
+        }
       }
-      sum = wave_reduce(sum, [](uint64_t p, uint64_t q) { return p + q; });
-      count = wave_reduce(count, [](uint32_t p, uint32_t q) { return p + q; });
-      if (lane == 0) {
-        l.list[s] = sum;
-        c->count[s] = count;
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q) {
+        sum[q] = wave_reduce(sum[q], [](uint64_t p, uint64_t r) { return p + r; });
+        count[q] = wave_reduce(count[q], [](uint32_t p, uint32_t r) { return p + r; });
       }
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q)
+        if (lane == 0 && s + q * kSampleWaves < segments) {
+          l.list[s + q * kSampleWaves] = sum[q];
+          c->count[s + q * kSampleWaves] = count[q];
+        }
     }
     __syncthreads();
     // the segments' last-code tokens that are kept are the first `ties` of all of them
@@ -693,9 +719,19 @@ template <class T> struct Sampler {
     uint64_t ranked = l.found[2];
     for (int64_t i = 0; i < per; ++i) {
       const int64_t o = ((int64_t)l.found[0] * per + i) * 64 + lane;
+      const Octet<uint16_t> oc = load_codes(o);
       uint64_t w[8], mine = 0;
       uint32_t mask;
-      octet(o, w, mask);
+      bool others;
+      octet(oc, w, mask, others);
+      if (others) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if ((int)(f2u(oc[j]) >> 16 & 0x7FFF) < base) {
+            w[j] = weigh(oc[j]);
+            if (w[j] < least) w[j] = 0;
+          }
+      }
       const uint32_t own = __popc(mask), upto_n = wave_scan(own, lane);
       uint64_t rank = ranked + upto_n - own;
 #pragma unroll
