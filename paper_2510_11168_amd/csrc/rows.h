@@ -137,10 +137,51 @@ template <> __device__ inline float load_one<float>(const float* p, int64_t i) {
 __device__ inline void store_one(uint16_t* p, int64_t i, float f) { p[i] = (uint16_t)pack_bf16(f, f); }
 __device__ inline void store_one(float* p, int64_t i, float f) { p[i] = f; }
 
+// Values of other lanes, word by word, by the vector ALU's own exchanges: through LDS (__shfl) each is a trip of some 60 clocks on a pipe that the CU's
+// waves share.  All lanes of the wave take part.
+template <class T, class F> __device__ inline T by_words(T v, F f) {
+  static_assert(sizeof(T) % 4 == 0, "whole words");
+  union { T t; uint32_t w[sizeof(T) / 4]; } x = {v}, y = {v};
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) y.w[i] = f(x.w[i]);
+  return y.t;
+}
+// Lanes M apart; for M = 4 and 8 a mirrored lane of the neighbouring M, which has the same once the steps below are done.
+template <int M, class T, class Op> __device__ inline T reduce_step(T v, Op op) {
+  if constexpr (M <= 8) {
+    return op(v, by_words(v, [](uint32_t w) {
+      constexpr int ctrl = M == 1 ? 0xB1 : M == 2 ? 0x4E : M == 4 ? 0x141 : 0x140;  // quad_perm 1 0 3 2, 2 3 0 1, row_half_mirror, row_mirror
+      return (uint32_t)__builtin_amdgcn_mov_dpp((int)w, ctrl, 0xF, 0xF, true);
+    }));
+  } else {                                               // (both halves of a swap of a value with itself: the even rows twice, the odd ones twice)
+    const auto swap = [](uint32_t w) { return M == 16 ? __builtin_amdgcn_permlane16_swap(w, w, false, false) : __builtin_amdgcn_permlane32_swap(w, w, false, false); };
+    return op(by_words(v, [&](uint32_t w) { return (uint32_t)swap(w)[0]; }), by_words(v, [&](uint32_t w) { return (uint32_t)swap(w)[1]; }));
+  }
+}
 // Reductions over a wave, or over each N of its lanes: every lane gets the result.
 template <int N = 64, class T, class Op> __device__ inline T wave_reduce(T v, Op op) {
-#pragma unroll
-  for (int m = N / 2; m; m >>= 1) v = op(v, __shfl_xor(v, m));
+  if constexpr (N >= 2) v = reduce_step<1>(v, op);
+  if constexpr (N >= 4) v = reduce_step<2>(v, op);
+  if constexpr (N >= 8) v = reduce_step<4>(v, op);
+  if constexpr (N >= 16) v = reduce_step<8>(v, op);
+  if constexpr (N >= 32) v = reduce_step<16>(v, op);
+  if constexpr (N >= 64) v = reduce_step<32>(v, op);
+  return v;
+}
+// One lane's value, for all; `lane` the same in all lanes.
+template <class T> __device__ inline T of_lane(T v, int lane) {
+  return by_words(v, [&](uint32_t w) { return (uint32_t)__builtin_amdgcn_readlane((int)w, lane); });
+}
+// Inclusive sums over a wave.
+template <class U> __device__ inline U wave_scan(U v) {
+#define ELMO_SCAN_STEP(ctrl, rows) v += by_words(v, [](uint32_t w) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, ctrl, rows, 0xF, false); })
+  ELMO_SCAN_STEP(0x111, 0xF);                            // row_shr 1, 2, 4, 8: nothing comes in at a row's begin
+  ELMO_SCAN_STEP(0x112, 0xF);
+  ELMO_SCAN_STEP(0x114, 0xF);
+  ELMO_SCAN_STEP(0x118, 0xF);
+  ELMO_SCAN_STEP(0x142, 0xA);                            // row_bcast 15: a row's sum to the next, odd ones
+  ELMO_SCAN_STEP(0x143, 0xC);                            // row_bcast 31
+#undef ELMO_SCAN_STEP
   return v;
 }
 // The waves' results of a workgroup, one a wave in `slots` behind a barrier (a lane reads one of them: sixteen held at once cost a kernel

@@ -99,23 +99,15 @@ __device__ inline uint64_t share_of(double part, uint64_t whole) {   // ceil(par
   return min(whole, max((uint64_t)1, (uint64_t)__builtin_ceil(part * (double)whole)));
 }
 
-template <class U> __device__ inline U wave_scan(U v, int lane) {    // inclusive
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const U other = __shfl_up(v, o);
-    if (lane >= o) v += other;
-  }
-  return v;
-}
 // Inclusive sums over the workgroup's threads, and their total.  Barriers before and behind the use of `slots`.
 template <class U> __device__ inline U block_scan(U v, U* slots, int wave, int lane, U& total) {
-  v = wave_scan(v, lane);
+  v = wave_scan(v);
   __syncthreads();
   if (lane == 63) slots[wave] = v;
   __syncthreads();
-  const U mine = lane < kSampleWaves ? slots[lane] : 0, upto = wave_scan(mine, lane);
-  total = __shfl(upto, kSampleWaves - 1);
-  return v + __shfl(upto - mine, wave);
+  const U mine = lane < kSampleWaves ? slots[lane] : 0, upto = wave_scan(mine);
+  total = of_lane(upto, kSampleWaves - 1);
+  return v + of_lane(upto - mine, __builtin_amdgcn_readfirstlane(wave));
 }
 // Falling order; `n` a power of two, by the whole workgroup.  Barriers before and behind.
 __device__ inline void sort_falling(uint64_t* s, int n, int tid) {
@@ -330,7 +322,7 @@ template <class T> struct Sampler {
         uint32_t c[4], sum = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum += c[i] = l.count[255 - 4 * lane - i];
-        uint32_t before = wave_scan(sum, lane) - sum;
+        uint32_t before = wave_scan(sum) - sum;
         if (lane == 63) l.found[0] = before + sum < left ? ~0ull : 0;      // fewer maxima than k: every token is taken
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -506,14 +498,14 @@ template <class T> struct Sampler {
     for (int64_t i = 0; i < per; ++i) {
       const int64_t o = ((int64_t)l.found[0] * per + i) * 64 + lane;
       uint64_t w[8];
-      const uint64_t mine = kept8(o, w), upto = wave_scan(mine, lane);
+      const uint64_t mine = kept8(o, w), upto = wave_scan(mine);
       uint64_t at = before + upto - mine;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (at <= want && at + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
         at += w[j];
       }
-      before += __shfl(upto, 63);
+      before += of_lane(upto, 63);
     }
   }
 
@@ -732,22 +724,22 @@ template <class T> struct Sampler {
             if (w[j] < least) w[j] = 0;
           }
       }
-      const uint32_t own = __popc(mask), upto_n = wave_scan(own, lane);
+      const uint32_t own = __popc(mask), upto_n = wave_scan(own);
       uint64_t rank = ranked + upto_n - own;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (mask >> j & 1) w[j] = rank++ < ties ? we : 0;
         mine += w[j];
       }
-      const uint64_t upto = wave_scan(mine, lane);
+      const uint64_t upto = wave_scan(mine);
       uint64_t here = at + upto - mine;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (here <= want && here + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
         here += w[j];
       }
-      at += __shfl(upto, 63);
-      ranked += __shfl(upto_n, 63);
+      at += of_lane(upto, 63);
+      ranked += of_lane(upto_n, 63);
     }
     return true;
   }
