@@ -54,8 +54,8 @@ __device__ inline Range part_of(int64_t octets, int part, int parts) {
 }
 
 // WHOLE: a row a workgroup.  It is read twice -- 256 rows of a large vocabulary that are worked on at a time fit the memory-side cache, from
-// which the second reading comes -- and the gradient goes past the caches.  4096 x 131072 BF16: 514 to 540 us, 4.0 TB/s of what has to move
-// (a copy: 4.8); rows held in registers, with the next one's loads under way as the gradient is written: 559 to 652.
+// which the second reading comes -- and the gradient goes past the caches.  4096 x 131072 BF16: 498 to 527 us, 4.1 to 4.3 TB/s of what has
+// to move (a copy: 4.8); rows held in registers, with the next one's loads under way as the gradient is written: 559 to 652.
 // SUMS, GRADIENT: few rows, in `parts` workgroups each: the parts' maxima and sums with the teacher's tokens' logits, then the gradient with them.  (The
 // second launch takes no logit that another part may already have overwritten.)  One row of 131072: see the launch.
 enum : int { DISTILL_WHOLE = 0, DISTILL_SUMS = 1, DISTILL_GRADIENT = 2 };

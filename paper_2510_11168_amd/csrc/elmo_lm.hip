@@ -245,11 +245,12 @@ extern "C" int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* 
 namespace {
 constexpr int64_t kMostV = ((int64_t)1 << 31) - 1;
 
-// Workgroups of a row without top-k: one where the rows fill the chip or are short.  Rows of 131072, top-p: 128 in FP32 72 us split (120 whole), 1 row 27
-// (109); in BF16, which one workgroup takes by codes, 128 rows 68 (58), 64 rows 51 (56), 1 row 28 (56).  One row of 16384 FP32: 25.8 (25.0).
-constexpr int64_t kSampleSplitRows = 128, kSampleSplitV = 16384;
+// Workgroups of a row without top-k: one where the rows fill the chip or are short.  Top-p, us, split and (a row more, or an element less) whole.  FP32:
+// 128 rows of 131072 70 and 118, one of 16384 20.9 and 22.5.  BF16, where one workgroup takes a row by codes in about half the time: 32 rows of 131072 36 and
+// 44, of 65536 30 and 28, one row of 65536 22 and 28; one of 32768 22.5 and 20.3; 64 rows of 131072 48 and 44.
+constexpr int64_t kSampleSplitRows = 128, kSampleSplitV = 16384, kSampleSplitRowsBf16 = 32, kSampleSplitVBf16 = 65536;
 int sample_parts(int64_t rows, int64_t V, bool bf16) {
-  if (rows > (bf16 ? kSampleSplitRows / 2 : kSampleSplitRows) || V < kSampleSplitV) return 1;
+  if (rows > (bf16 ? kSampleSplitRowsBf16 : kSampleSplitRows) || V < (bf16 ? kSampleSplitVBf16 : kSampleSplitV)) return 1;
   return (int)std::min<int64_t>(std::min<int64_t>(64, (V + 4095) / 4096), std::max<int64_t>(2, 256 / rows));
 }
 template <class T, int STEP> int launch_sample_step(const elmo::SampleArgs& a, unsigned grid, hipStream_t st) {
@@ -303,8 +304,8 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
 }
 
 namespace {
-// Workgroups of a row: one where the rows fill the chip or are short, else up to 64, each with at least one round of octets (131072 BF16: 1 row 10.4 us,
-// 128 rows 25.7, 129 rows, a workgroup each, 34).
+// Workgroups of a row: one where the rows fill the chip or are short, else up to 64, each with at least one round of octets (131072 BF16: 1 row 9 - 11 us,
+// 128 rows 24.0, 129 rows, a workgroup each, 31.0).
 int distill_parts(int64_t rows, int64_t V) {
   const int64_t rounds = (V / 8 + elmo::kDistillThreads - 1) / elmo::kDistillThreads;
   if (rows > 128 || rounds < 4) return 1;

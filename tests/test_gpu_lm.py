@@ -314,7 +314,7 @@ def test_sample_rows_of_few_values(b, V, dtype):
         check_tokens(z, u, token.cpu(), prob.cpu(), **s)
 
 
-@pytest.mark.parametrize("rows,V", [(130, 20011), (3, 16384), (129, 16391)])
+@pytest.mark.parametrize("rows,V", [(130, 20011), (3, 16384), (129, 16391), (9, 65543)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_sample_without_top_k_in_one_workgroup_and_in_several(b, rows, V, dtype):
     """Rows on both sides of the number from which a row is no longer split; among them empty ones, ones of infinities, of zeros, of one
