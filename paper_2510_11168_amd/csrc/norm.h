@@ -227,7 +227,8 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm_back(NormBackArg
         both[1] += s_red[phase][slot][i][1];
       }
     }
-    const float R = 1.0f / sqrtf(both[0] / (float)a.d + a.eps), k = R * R * R * (both[1] / (float)a.d);
+    // (R^3 leaves FP32 long before the gradient does: each factor R stands beside one that it brings back into range)
+    const float R = 1.0f / sqrtf(both[0] / (float)a.d + a.eps), along = R * (both[1] / (float)a.d);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c = c0 + s * STEP;
@@ -235,10 +236,10 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm_back(NormBackArg
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float g = go[s][i] * w[s][i];
-          f[i] = g * R - ho[s][i] * k;
+          const float g = go[s][i] * w[s][i], hR = ho[s][i] * R;
+          f[i] = R * (g - hR * along);
           if (a.dsum) f[i] += so[s][i];
-          dw[s][i] = __builtin_fmaf(go[s][i] * R, ho[s][i], dw[s][i]);
+          dw[s][i] = __builtin_fmaf(go[s][i], hR, dw[s][i]);
         }
         store_octet((T*)a.dh + row * a.dhs + c, a.d - c, f);
       }

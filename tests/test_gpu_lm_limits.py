@@ -1,0 +1,75 @@
+"""The output-end operators where their numbers, sizes or workspaces are at an end of what the header allows, against the 64-bit statements.
+
+Tolerances in the units of test_gpu_lm.py: E = 2^-24 (half a step of FP32, relative), HALF = half a step of the output type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import lm_oracle as o
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+E = 2.0 ** -24
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: E}
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2510_11168_amd import binding
+    return binding
+
+
+def f64(t):
+    return t.to(torch.float64).cpu().numpy()
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def close(got, want, tol, what):
+    assert np.all(np.isfinite(f64(got))), what
+    err = np.abs(f64(got) - want)
+    assert np.all(err <= tol), f"{what}: {float(np.max(err / tol)):.3g} times the tolerance"
+
+
+# ------------------------------------------------------------------ norm
+def back_tolerances(dy, h, w, eps, dtype, want):
+    """A lane adds at most 64 terms, the tree and the waves 24 levels: n = 88 additions on the way of a term.  R has half the relative error of the
+    sum of squares, all of its terms positive, (n / 2) e, and 8 e of its own; h R^3 mean(g h) has R three times, the sum of g h (n e of the sum of
+    magnitudes) and 12 e of products.  A weight gradient adds rows / 512 terms of a team, 3 teams, 8 shares and 6 levels at most."""
+    H, G, n = f64(h), f64(dy) * f64(w), 88
+    R = 1 / np.sqrt(np.mean(H * H, axis=1, keepdims=True) + eps)
+    along = np.mean(np.abs(G * H), axis=1, keepdims=True)
+    th = E * ((n / 2 + 8) * np.abs(G * R) + np.abs(H) * R ** 3 * along * (2.5 * n + 12)) + (HALF[dtype] + E) * np.abs(want) + 1e-38
+    tw = E * (n / 2 + 8 + len(H) / 512 + 17) * np.sum(np.abs(f64(dy) * H * R), axis=0) + 1e-38
+    return th, tw
+
+
+@pytest.mark.parametrize("rms,eps", [(1e-15, 0.0), (1e-13, 1e-30), (1e14, 1e-6), (1e16, 1e-6)])
+@pytest.mark.parametrize("rows,d", [(5, 1001), (3, 2048), (2, 9000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_backward_of_large_and_small_rows(b, rows, d, dtype, rms, eps):
+    """A gradient that goes mostly along h: what the projection takes away is of its size."""
+    g = gen(d)
+    h = (rms * torch.randn((rows, d), generator=g)).to(dtype)
+    dy = (h.float() / rms + 0.1 * torch.randn((rows, d), generator=g)).to(dtype)
+    w = (1 + 0.1 * torch.randn(d, generator=g)).to(dtype)
+    dh, dw = torch.empty((rows, d), dtype=dtype, device=DEV), torch.empty(d, device=DEV)
+    b.elmo_rms_norm_backward(dy.to(DEV), h.to(DEV), dh, w.to(DEV), eps, dweight=dw)
+    want, wantw = o.rms_norm_backward(f64(dy), f64(h), f64(w), eps)
+    th, tw = back_tolerances(dy, h, w, eps, dtype, want)
+    close(dh, want, th, "dh")
+    close(dw, wantw, tw, "dweight")
+
+
+def test_norm_backward_of_zeros_and_a_very_small_eps(b):
+    h, dy = torch.zeros((2, 300), device=DEV), torch.randn((2, 300), generator=gen(1)).to(DEV)
+    dh, dw = torch.empty_like(h), torch.empty(300, device=DEV)
+    b.elmo_rms_norm_backward(dy, h, dh, None, 1e-28, dweight=dw)
+    want = f64(dy) / np.sqrt(np.float64(np.float32(1e-28)))
+    close(dh, want, 4 * E * np.abs(want), "dh")
+    assert not dw.any()
