@@ -234,8 +234,8 @@ void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t o
  * with a scale per row in scale_out [rows]: with p = weight * h and m = max |p| of the row
  *   ELMO_INT8:      y = round(127 p / m),       scale = m / (127 sqrt(mean(h^2) + eps))
  *   ELMO_FP8_E4M3:  y = round_E4M3(448 p / m),  scale = m / (448 sqrt(mean(h^2) + eps))
- * so that y * scale is the norm; the quotient is p * (127 * (1 / m)), p exact and three FP64 roundings.  A row of zeros gives zeros and scale 0; a row that holds an infinity or NaN, or squares beyond FP32,
- * gives zeros and scale NaN.  sum_out may be x or residual, and y the other of the two, where address, stride and dtype are the same. */
+ * so that y * scale is the norm; the quotient is p * (127 * (1 / m)), p exact and three FP64 roundings.  A row of zeros gives zeros and scale 0; a row that holds an infinity or NaN, or whose squares
+ * add up to more than FP32 holds, gives zeros and scale NaN (BF16 and FP32 rows of such squares are normalised as any others).  sum_out may be x or residual, and y the other of the two, where address, stride and dtype are the same. */
 int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int64_t d, const void* residual,
                   int64_t residual_stride, const void* weight, int weight_dtype, float eps, void* sum_out,
                   int64_t sum_stride, void* y, int64_t y_stride, int y_dtype, float* scale_out, void* hip_stream);
@@ -243,7 +243,7 @@ int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int6
 /* Its backward pass.  h: what was normalised (sum_out, or x without a residual).  With R = 1 / sqrt(mean(h^2) + eps), g = weight * dy:
  *   dh = R (g - h R^2 mean(g h)) + dsum      (the gradient of x and of the residual alike)
  *   dweight[j] = sum over rows of R dy h     (FP32 [d], overwritten; NULL = not wanted; zeros for no rows)
- * dsum (NULL = none) is the gradient that reaches sum_out from elsewhere.  dh may be dy, h or dsum where address and stride are
+ * R itself has to lie within FP32.  dsum (NULL = none) is the gradient that reaches sum_out from elsewhere.  dh may be dy, h or dsum where address and stride are
  * the same.  dweight needs a workspace of elmo_rms_norm_backward_bytes(rows, d) bytes, 4-byte aligned. */
 size_t elmo_rms_norm_backward_bytes(int64_t rows, int64_t d);
 int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int64_t h_stride, int dtype, int64_t rows,

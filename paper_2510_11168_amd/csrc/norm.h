@@ -6,6 +6,9 @@
 // on p and m alone.  Both are exact in FP64 (24 x 24 bits), the maximum does not depend on an order, and what is left is 127 (1 / m), two FP64 roundings a row,
 // and one product an element: the same numbers whichever way a row is split over lanes.  The scale is m R / 127 (448 for E4M3).
 //
+// Squares are summed in FP32.  A row whose sum leaves that type's range while its elements are inside is summed once more, times a power of two
+// (out_of_range, scale_into_range): the same row as any other but for that.
+//
 // Bound: memory.  A row is read once and stays in registers, S octets a lane, spread over WPR waves.
 #pragma once
 #include "rows.h"
@@ -25,6 +28,12 @@ struct NormArgs {
   float eps;
   bool w32;                          // FP32 weights
 };
+
+// Mean square `ms` (NaN among them) of a row that has to be summed again.  2^-100: what lies below has lost more than the last bit of squares below 2^-126;
+// with that much eps it does not matter.
+__device__ inline bool out_of_range(float ms, float eps, bool large) { return !(ms + eps >= 0x1p-100f && (ms < __builtin_inff() || !large)); }
+// Elements up to 2^-43 come to 2^53, the least ones (2^-149) to 2^-53; elements up to 2^128 to 2^48.  Squares and their sums stay inside either way.
+__device__ inline float scale_into_range(float ms) { return ms < 1.0f ? 0x1p96f : 0x1p-80f; }
 
 // Octet of the weights; 1 without weights.
 __device__ inline void load_weights(const void* w, bool w32, int c, int valid, float (&f)[8]) {
@@ -91,7 +100,24 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm(NormArgs a) {
     }
   }
   sq = row_reduce<WPR>(sq, s_sum[slot], in_row, lane, [](float p, float q) { return p + q; });
-  const float ms = sq / (float)a.d, rstd = 1.0f / sqrtf(ms + a.eps);
+  float ms = sq / (float)a.d, eps = a.eps;
+  if (out_of_range(ms, eps, !EIGHT)) {                    // (the same for all lanes of a row; 8-bit rows of too large squares have no scale)
+    const float up = scale_into_range(ms);
+    sq = 0.0f;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if (c0 + s * STEP < a.d) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[s][i] *= up;
+          sq = __builtin_fmaf(h[s][i], h[s][i], sq);
+        }
+      }
+    if (WPR > 1) __syncthreads();                         // (the slots have been read)
+    ms = row_reduce<WPR>(sq, s_sum[slot], in_row, lane, [](float p, float q) { return p + q; }) / (float)a.d;
+    eps = eps * up * up;
+  }
+  const float rstd = 1.0f / sqrtf(ms + eps);
 
   if constexpr (!EIGHT) {
     using O = typename std::conditional<OUT == OUT_BF16, uint16_t, float>::type;
@@ -204,31 +230,43 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_rms_norm_back(NormBackArg
         if (a.dsum) so[s] = load_octet((const T*)a.dsum + row * a.dss + c, a.d - c);
       }
     }
-    f32x2 both = {0.0f, 0.0f};       // sum of h^2, sum of g h
+    const auto means = [&](float up) {               // of h^2 and g h, with h times `up`
+      f32x2 both = {0.0f, 0.0f};
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-      if (c0 + s * STEP < a.d) {
+      for (int s = 0; s < S; ++s)
+        if (c0 + s * STEP < a.d) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          both[0] = __builtin_fmaf(ho[s][i], ho[s][i], both[0]);
-          both[1] = __builtin_fmaf(go[s][i] * w[s][i], ho[s][i], both[1]);
+          for (int i = 0; i < 8; ++i) {
+            const float hi = ho[s][i] * up;
+            both[0] = __builtin_fmaf(hi, hi, both[0]);
+            both[1] = __builtin_fmaf(go[s][i] * w[s][i], hi, both[1]);
+          }
+        }
+      both[0] = wave_sum(both[0]);
+      both[1] = wave_sum(both[1]);
+      if constexpr (WPR > 1) {
+        // two sets of slots: a wave that is a row ahead writes the other one, and two rows ahead lies behind the next barrier
+        if (lane == 0) s_red[phase][slot][in_row] = both;
+        __syncthreads();
+        both = s_red[phase][slot][0];
+#pragma unroll
+        for (int i = 1; i < WPR; ++i) {
+          both[0] += s_red[phase][slot][i][0];
+          both[1] += s_red[phase][slot][i][1];
         }
       }
-    both[0] = wave_sum(both[0]);
-    both[1] = wave_sum(both[1]);
-    if constexpr (WPR > 1) {
-      // two sets of slots: a wave that is a row ahead writes the other one, and two rows ahead lies behind the next barrier
-      if (lane == 0) s_red[phase][slot][in_row] = both;
-      __syncthreads();
-      both = s_red[phase][slot][0];
-#pragma unroll
-      for (int i = 1; i < WPR; ++i) {
-        both[0] += s_red[phase][slot][i][0];
-        both[1] += s_red[phase][slot][i][1];
-      }
+      return f32x2{both[0] / (float)a.d, both[1] / (float)a.d};
+    };
+    f32x2 mean = means(1.0f);
+    float eps = a.eps, up = 1.0f;
+    if (out_of_range(mean[0], eps, true)) {
+      up = scale_into_range(mean[0]);
+      if (WPR > 1) __syncthreads();  // (the slots have been read)
+      mean = means(up);
+      eps = eps * up * up;
     }
     // (R^3 leaves FP32 long before the gradient does: each factor R stands beside one that it brings back into range)
-    const float R = 1.0f / sqrtf(both[0] / (float)a.d + a.eps), along = R * (both[1] / (float)a.d);
+    const float Rup = 1.0f / sqrtf(mean[0] + eps), along = Rup * mean[1], R = Rup * up;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int c = c0 + s * STEP;

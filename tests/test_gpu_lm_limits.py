@@ -37,6 +37,35 @@ def close(got, want, tol, what):
 
 
 # ------------------------------------------------------------------ norm
+@pytest.mark.parametrize("rms,eps", [(1e-36, 0.0), (1e-25, 0.0), (1e-20, 1e-38), (1e-8, 1e-16), (1e16, 1e-6), (1e18, 1e-6), (1e30, 1e-6), (4e37, 0.0)])
+@pytest.mark.parametrize("rows,d", [(3, 8), (5, 1001), (3, 2048), (2, 9000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_of_rows_whose_squares_leave_fp32(b, rows, d, dtype, rms, eps):
+    g = gen(d + 1)
+    x, r = (rms * torch.randn((rows, d), generator=g)).to(dtype), (rms * torch.randn((rows, d), generator=g)).to(dtype)
+    x[0], r[0] = torch.sign(x[0].float()).to(dtype), 0       # an ordinary row beside them
+    w = (1 + 0.1 * torch.randn(d, generator=g)).to(dtype)
+    h32 = x.float() + r.float()
+    assert bool(torch.isfinite(h32).all())
+    want, h64, root = o.rms_norm(f64(x), f64(w), float(np.float32(eps)), f64(r))
+    # as in back_tolerances: half of a sum of n = 88 additions on the way, a root, a quotient and two products
+    rel = (88 / 2 + 11) * E
+    args = x.to(DEV), r.to(DEV), w.to(DEV)
+    for out in (torch.bfloat16, torch.float32):
+        y, s = torch.empty((rows, d), dtype=out, device=DEV), torch.empty((rows, d), dtype=dtype, device=DEV)
+        b.elmo_rms_norm(args[0], y, args[2], eps, residual=args[1], sum_out=s)
+        # the sum's own rounding to FP32 is E of it
+        close(y, want, (HALF[out] + rel) * np.abs(want) + 3 * E * np.abs(f64(w) * h64 / root) + 1e-38, "y")
+        assert torch.equal(s.cpu(), h32.to(dtype)), "the stream is the rounded sum"
+    q, scale = torch.empty((rows, d), dtype=torch.int8, device=DEV), torch.empty(rows, device=DEV)
+    b.elmo_rms_norm(args[0], q, args[2], eps, residual=args[1], scale_out=scale)
+    quotients, m = o.rows_in_8_bits(h32.numpy(), f64(w), 127)
+    finite = f64(h32 * h32).sum(axis=1) < 3.4e38
+    assert np.array_equal(q.cpu().numpy(), np.where(finite[:, None], np.rint(quotients), 0).astype(np.int8))
+    assert not np.isfinite(f64(scale)[~finite]).any()
+    close(scale[torch.from_numpy(finite)], (m / (127 * root))[finite, 0], (rel + 2 * E) * (m / (127 * root))[finite, 0], "scale")
+
+
 def back_tolerances(dy, h, w, eps, dtype, want):
     """A lane adds at most 64 terms, the tree and the waves 24 levels: n = 88 additions on the way of a term.  R has half the relative error of the
     sum of squares, all of its terms positive, (n / 2) e, and 8 e of its own; h R^3 mean(g h) has R three times, the sum of g h (n e of the sum of
@@ -49,7 +78,7 @@ def back_tolerances(dy, h, w, eps, dtype, want):
     return th, tw
 
 
-@pytest.mark.parametrize("rms,eps", [(1e-15, 0.0), (1e-13, 1e-30), (1e14, 1e-6), (1e16, 1e-6)])
+@pytest.mark.parametrize("rms,eps", [(1e-15, 0.0), (1e-13, 1e-30), (1e14, 1e-6), (1e16, 1e-6), (1e18, 1e-6), (1e30, 1e-6), (1e37, 0.0), (1e-25, 0.0), (1e-36, 0.0)])
 @pytest.mark.parametrize("rows,d", [(5, 1001), (3, 2048), (2, 9000)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_norm_backward_of_large_and_small_rows(b, rows, d, dtype, rms, eps):
