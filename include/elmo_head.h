@@ -266,10 +266,10 @@ int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, co
  * temperature, top_k, top_p, min_p: one value a row, or NULL (1, off, off, off).  temperature <= 0 or NaN: the largest logit, lowest
  * index.  top_k < 1, top_p >= 1 or NaN, min_p <= 0 or NaN: off; top_p <= 0 keeps one token, min_p >= 1 those equal to the largest.  u is
  * clamped to [0, 1), NaN counts as 0.  Logits of -infinity and NaN are never drawn; beside logits of +infinity nothing else is.
- * Weights are whole multiples of 2^-F of the largest, F = min(50, 62 - ceil(log2 V)), computed in FP64 (a token below half of that
- * is never drawn), and their sums are exact: the token does not depend on how a row is split.
- * idx_out [rows]: the token, -1 where a row has none; prob_out [rows] (NULL = not wanted): its share of the kept weight, 0 where there
- * is none.  workspace: elmo_sample_bytes(rows, V) bytes, 256-byte aligned (NULL if that is 0, and with top_k). */
+ * Weights are whole multiples of 2^-F of the largest, F = min(50, 62 - ceil(log2 V)), rounded to nearest from FP64 values that are right to 2^-51 (a
+ * token below half a multiple is never drawn), and their sums are exact: the token does not depend on how a row is split.
+ * idx_out [rows]: the token, -1 where a row has none; prob_out [rows] (NULL = not wanted): its share of the kept weight, from
+ * its FP64 weight, 0 where there is none.  workspace: elmo_sample_bytes(rows, V) bytes, 256-byte aligned (NULL if that is 0, and with top_k). */
 size_t elmo_sample_bytes(int64_t rows, int64_t V);
 int elmo_sample(const void* logits, int64_t logits_stride, int dtype, int64_t rows, int64_t V, const float* u,
                 const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* idx_out,

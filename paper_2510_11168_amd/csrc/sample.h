@@ -5,7 +5,8 @@
 // smallest weight.  The token is the first one in order of index at which the kept weight so far exceeds u times the kept weight.
 //
 // Which token a number falls on is decided next to borders, so the weights are whole numbers, W = round(2^F exp((z - max z) / t)) from FP64, with
-// F such that a row's sum stays below 2^63: sums are exact in any order and any split of a row gives the same token.
+// F such that a row's sum stays below 2^63: sums are exact in any order and any split of a row gives the same token.  A token's share is its FP64
+// weight over that sum: few bits of a light token's W are left.
 //
 // Bound: a row is read two to four times, by one workgroup, and stays in the caches for the second time on; where many tokens are kept it is the
 // weights' arithmetic (some twenty FP64 and integer instructions each).  BF16 256 x 131072: top-p 54 us, no filter (no counts) 39, greedy (two plain
@@ -52,7 +53,8 @@ __device__ inline float of_key(uint32_t k) { return u2f((int32_t)k < 0 ? k & 0x7
 __device__ inline uint64_t place_of(float z, int64_t index) { return (uint64_t)key_of(z) << 32 | (uint32_t)~(uint32_t)index; }
 
 // Weight of a logit: y = (z - M) 256 log2(e) / t = n + r, 2^(n / 256) by a table of the 256 roots and the exponent, 2^(r / 256) by its series up to
-// r^3 (the next term is below 2^-42).  NaN and -infinity end at the lower bound, which rounds to no weight.
+// r^4 (the next term is below 2^-54; roundings of y, root, series and product: 2^-51 of the weight together).  NaN and -infinity end at the lower bound,
+// which rounds to no weight.
 struct Weigh {
   const double* roots;                         // 2^(i / 256), in LDS
   double M, k, least;                          // maximum, 256 log2(e) / t, lower bound of y
@@ -63,13 +65,15 @@ struct Weigh {
     r = y - (s - magic);
     return (int)(uint32_t)__double_as_longlong(s);
   }
-  __device__ inline uint64_t operator()(float z, int& n) const {
+  __device__ inline double unrounded(float z, int& n) const {
     constexpr double c = 0.6931471805599453 / 256;
     double r;
     n = steps(__builtin_fmax(((double)z - M) * k, least), r);
-    const double p = __builtin_fma(__builtin_fma(__builtin_fma(c * c * c / 6, r, c * c / 2), r, c), r, 1.0);
-    const double w = __builtin_ldexp(p * roots[n & 255], (n >> 8) + F);
-    return (uint64_t)__double_as_longlong(w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52: rounded to a whole number
+    const double p = __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(c * c * c * c / 24, r, c * c * c / 6), r, c * c / 2), r, c), r, 1.0);
+    return __builtin_ldexp(p * roots[n & 255], (n >> 8) + F);
+  }
+  __device__ inline uint64_t operator()(float z, int& n) const {
+    return (uint64_t)__double_as_longlong(unrounded(z, n) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52: rounded to a whole number
   }
   __device__ inline uint64_t operator()(float z) const { int n; return (*this)(z, n); }
   __device__ inline int bin(int n) const { return min(-n >> 2, kSampleBins - 1); }        // 0: the largest weights
@@ -213,6 +217,13 @@ template <class T> struct Sampler {
   __device__ __forceinline__ void answer(int64_t token, float prob) const {
     a.token[row] = (int32_t)token;
     if (a.prob) a.prob[row] = prob;
+  }
+  __device__ __forceinline__ void drawn(int64_t token, float logit, uint64_t all) const {
+    int n;
+    answer(token, a.prob ? (float)(weigh.unrounded(logit, n) / (double)all) : 0.0f);
+  }
+  __device__ __forceinline__ float logit_of(int64_t token) const {        // of one that has a weight
+    return infinite ? 0.0f : load_one(z, token);
   }
   __device__ __forceinline__ uint64_t number(uint64_t all) const {        // u of the kept weight
     const uint64_t want = (uint64_t)(rs.u * (double)all);
@@ -365,7 +376,7 @@ template <class T> struct Sampler {
       });
       __syncthreads();
       const uint64_t before = tid < nk ? l.mass[kSampleShortK + tid] : 0;
-      if (kept && before <= want && before + w > want) answer((int64_t)(uint32_t)~(uint32_t)place, (float)((double)w / (double)all));
+      if (kept && before <= want && before + w > want) drawn((int64_t)(uint32_t)~(uint32_t)place, of_key(place >> 32), all);
       return true;
     }
     sort_falling(l.list, kSampleShortK, tid);
@@ -373,7 +384,8 @@ template <class T> struct Sampler {
     // (an entry of 0 would be index 2^32 - 1, which no row has)
     const uint64_t wi = entry ? l.mass[(uint32_t)entry] : 0;
     const uint64_t by_index = block_scan(wi, l.sum, wave, lane, all);
-    if (wi && by_index > want && by_index - wi <= want) answer((int64_t)(uint32_t)~(uint32_t)(entry >> 32), (float)((double)wi / (double)all));
+    const int64_t token = (int64_t)(uint32_t)~(uint32_t)(entry >> 32);
+    if (wi && by_index > want && by_index - wi <= want) drawn(token, logit_of(token), all);
     return true;
   }
 
@@ -503,7 +515,7 @@ template <class T> struct Sampler {
       uint64_t at = before + upto - mine;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (at <= want && at + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
+        if (at <= want && at + w[j] > want) drawn(o * 8 + j, logit_of(o * 8 + j), all);
         at += w[j];
       }
       before += of_lane(upto, 63);
@@ -736,7 +748,7 @@ template <class T> struct Sampler {
       uint64_t here = at + upto - mine;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (here <= want && here + w[j] > want) answer(o * 8 + j, (float)((double)w[j] / (double)all));
+        if (here <= want && here + w[j] > want) drawn(o * 8 + j, oc[j], all);
         here += w[j];
       }
       at += of_lane(upto, 63);

@@ -102,3 +102,63 @@ def test_norm_backward_of_zeros_and_a_very_small_eps(b):
     want = f64(dy) / np.sqrt(np.float64(np.float32(1e-28)))
     close(dh, want, 4 * E * np.abs(want), "dh")
     assert not dw.any()
+
+
+# ------------------------------------------------------------------ sampling
+def draw(b, z, u, **kw):
+    token, prob = torch.full((len(u),), -7, dtype=torch.int32, device=DEV), torch.full((len(u),), -7.0, device=DEV)
+    b.elmo_sample(z.to(DEV), u.to(DEV), token, prob_out=prob, **{k: v.to(DEV) for k, v in kw.items()})
+    return token.cpu(), prob.cpu()
+
+
+@pytest.mark.parametrize("rows,V", [(3, 700), (3, 20011), (2, 131072), (140, 20000)])
+@pytest.mark.parametrize("top_k", [0, 60, 400, 600])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_share_of_a_light_token(b, rows, V, top_k, dtype):
+    """u = 0 draws the first kept token, however light: its share has FP32's bits also where a few units of 2^-F are all it weighs."""
+    g = gen(V)
+    F = min(50, 62 - (V - 1).bit_length())
+    z = torch.full((rows, V), -float("inf"))
+    live = min(V - 2, 300)                                   # constrained decoding: most tokens are masked
+    for r in range(rows):
+        z[r, 1 + torch.randperm(V - 1, generator=g)[:live]] = 4 * torch.rand(live, generator=g) - 4
+        z[r, V - 1 - r % 3] = 0.0
+        z[r, 0] = -[10.0, 24.0, 0.69 * (F - 2)][r % 3]       # the last: a weight of about four units
+    z = z.to(dtype)
+    if top_k == 60:                                          # a list that ends within the tokens: of few live ones
+        z[:, 1:V - 3][torch.rand((rows, V - 4), generator=g) < 0.9] = -float("inf")
+    kw = dict(top_k=torch.full((rows,), top_k, dtype=torch.int32)) if top_k else {}
+    token, prob = draw(b, z, torch.zeros(rows), **kw)
+    assert not token.any()
+    w = np.exp(f64(z))                                       # (the largest logit is 0)
+    share = w[:, 0] / w.sum(axis=1)
+    # one rounding to FP32, the FP64 weight's 2^-51, half a unit of 2^-F for each of the sum's tokens
+    close(prob, share, share * (E + 2.0 ** -50 + (live + 3) * 2.0 ** -(F + 1)), "share")
+
+
+def test_borders_between_two_tokens(b):
+    """Temperatures for which the border between two tokens lies 2^-50 to 2^-46 beside a number: the token on the number's side is drawn.  The weight of
+    the lighter one is right to 2^-51 and half a unit of 2^-50, the border then to 2^-52, and u times the sum is rounded by 2^-53."""
+    ts, us, zs, want = [], [], [], []
+    for z in (-1.0, -2.0, -3.0):
+        for start in (0x3E800000, 0x3F000000, 0x3F800000, 0x40000000):       # 1/4, 1/2, 1, 2
+            t = np.arange(start, start + (1 << 23), dtype=np.uint32).view(np.float32)
+            border = 1 / (1 + np.exp(z / t.astype(np.float64)))
+            u = border.astype(np.float32)
+            off = np.abs(border - u.astype(np.float64))
+            at = np.flatnonzero((off > 2.0 ** -50.1) & (off < 2.0 ** -45.9))
+            exact = 1 / (1 + np.exp(np.longdouble(z) / t[at].astype(np.longdouble)))
+            for i, e in zip(at, exact):
+                d = float(u[i].astype(np.longdouble) - e)
+                if 2.0 ** -50 <= abs(d) <= 2.0 ** -46:
+                    ts.append(float(t[i])), us.append(float(u[i])), zs.append(z), want.append(int(d >= 0))
+    assert len(want) >= 20 and 0 < sum(want) < len(want)
+    t, u = torch.tensor(ts), torch.tensor(us)
+    for dtype in (torch.bfloat16, torch.float32):
+        rows = torch.tensor([[0.0, z, -float("inf")] for z in zs]).to(dtype)
+        for kw in ({}, dict(top_k=torch.full((len(ts),), 2, dtype=torch.int32))):
+            for order in (rows, rows[:, [2, 0, 1]]):
+                token, _ = draw(b, order, u, temperature=t, **kw)
+                first = 0 if order is rows else 1
+                wrong = np.flatnonzero(token.numpy() - first != np.array(want))
+                assert not len(wrong), (dtype, list(kw), len(wrong), "of", len(want))
