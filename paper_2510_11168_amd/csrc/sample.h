@@ -72,9 +72,11 @@ struct Weigh {
     const double p = __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(c * c * c * c / 24, r, c * c * c / 6), r, c * c / 2), r, c), r, 1.0);
     return __builtin_ldexp(p * roots[n & 255], (n >> 8) + F);
   }
-  __device__ inline uint64_t operator()(float z, int& n) const {
-    return (uint64_t)__double_as_longlong(unrounded(z, n) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;   // + 2^52: rounded to a whole number
+  __device__ inline double unrounded(float z) const { int n; return unrounded(z, n); }
+  static __device__ inline uint64_t whole(double w) {
+    return (uint64_t)__double_as_longlong(w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;         // + 2^52: rounded to a whole number
   }
+  __device__ inline uint64_t operator()(float z, int& n) const { return whole(unrounded(z, n)); }
   __device__ inline uint64_t operator()(float z) const { int n; return (*this)(z, n); }
   __device__ inline int bin(int n) const { return min(-n >> 2, kSampleBins - 1); }        // 0: the largest weights
 };
@@ -220,10 +222,7 @@ template <class T> struct Sampler {
     a.token[row] = (int32_t)token;
     if (a.prob) a.prob[row] = prob;
   }
-  __device__ __forceinline__ void drawn(int64_t token, float logit, uint64_t all) const {
-    int n;
-    answer(token, a.prob ? (float)(weigh.unrounded(logit, n) / (double)all) : 0.0f);
-  }
+  __device__ __forceinline__ void drawn(int64_t token, double weight, uint64_t all) const { answer(token, (float)(weight / (double)all)); }
   __device__ __forceinline__ float logit_of(int64_t token) const {        // of one that has a weight
     return infinite ? 0.0f : load_one(z, token);
   }
@@ -356,7 +355,9 @@ template <class T> struct Sampler {
     if (n > kSampleList) return false;
     order_list(n);
     const int nk = (int)min((int64_t)n, rs.k);           // at most 512: one a thread
-    const uint64_t place = tid < nk ? l.list[tid] : 0, w = tid < nk ? weigh(of_key(place >> 32)) : 0;
+    const uint64_t place = tid < nk ? l.list[tid] : 0;
+    const double exact = tid < nk ? weigh.unrounded(of_key(place >> 32)) : 0.0;
+    const uint64_t w = Weigh::whole(exact);
     uint64_t total, all;
     const uint64_t upto = block_scan(w, l.sum, wave, lane, total);
     const bool kept = w >= least && (rs.p >= 1.0 || upto - w < share_of(rs.p, total));
@@ -378,7 +379,7 @@ template <class T> struct Sampler {
       });
       __syncthreads();
       const uint64_t before = tid < nk ? l.mass[kSampleShortK + tid] : 0;
-      if (kept && before <= want && before + w > want) drawn((int64_t)(uint32_t)~(uint32_t)place, of_key(place >> 32), all);
+      if (kept && before <= want && before + w > want) drawn((int64_t)(uint32_t)~(uint32_t)place, exact, all);
       return true;
     }
     sort_falling(l.list, kSampleShortK, tid);
@@ -387,7 +388,7 @@ template <class T> struct Sampler {
     const uint64_t wi = entry ? l.mass[(uint32_t)entry] : 0;
     const uint64_t by_index = block_scan(wi, l.sum, wave, lane, all);
     const int64_t token = (int64_t)(uint32_t)~(uint32_t)(entry >> 32);
-    if (wi && by_index > want && by_index - wi <= want) drawn(token, logit_of(token), all);
+    if (wi && by_index > want && by_index - wi <= want) drawn(token, weigh.unrounded(logit_of(token)), all);
     return true;
   }
 
@@ -517,7 +518,7 @@ template <class T> struct Sampler {
       uint64_t at = before + upto - mine;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (at <= want && at + w[j] > want) drawn(o * 8 + j, logit_of(o * 8 + j), all);
+        if (at <= want && at + w[j] > want) drawn(o * 8 + j, weigh.unrounded(logit_of(o * 8 + j)), all);
         at += w[j];
       }
       before += of_lane(upto, 63);
@@ -750,7 +751,7 @@ template <class T> struct Sampler {
       uint64_t here = at + upto - mine;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (here <= want && here + w[j] > want) drawn(o * 8 + j, oc[j], all);
+        if (here <= want && here + w[j] > want) drawn(o * 8 + j, weigh.unrounded(oc[j]), all);
         here += w[j];
       }
       at += of_lane(upto, 63);
