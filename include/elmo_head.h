@@ -254,10 +254,12 @@ int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int
 /* 8-bit integer product with a scale for each row of either operand (token and output channel):
  *   out[m, n] = (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]
  * a [M, K] and b [N, K] int8 (all 256 values), scales and bias FP32 (bias NULL = none), out [M, N] in out_dtype.  The sum is exact
- * (0 <= K <= 131071; of no products it is 0).  M and N up to 2^30. */
+ * (0 <= K <= 131071; of no products it is 0).  M and N up to 2^30, fewer than 2^23 tiles of 256 x 256 outputs.
+ * elmo_int8_matmul_tile: how these sizes are worked on, in tiles of 64, 128 or 256, or 0 for the kernel of few tokens that streams the weights (-1: refused). */
 int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, const int8_t* b, int64_t b_stride,
                      const float* b_scale, const float* bias, int64_t M, int64_t N, int64_t K, void* out,
                      int64_t out_stride, int out_dtype, void* hip_stream);
+int elmo_int8_matmul_tile(int64_t M, int64_t N, int64_t K);
 
 /* One token for each row of V logits (1 <= V < 2^31), from a given random number u[row] in [0, 1).  Tokens are ordered by (logit
  * falling, index rising) and weigh exp((z - max z) / temperature).  Kept are the first top_k of them, of those the shortest beginning

@@ -94,6 +94,8 @@ _lib.elmo_rms_norm_backward.restype = _I
 _lib.elmo_rms_norm_backward.argtypes = [_P, _L, _P, _L, _I, _L, _L, _P, _I, _F, _P, _L, _P, _L, _P, _P, _Z, _P]
 _lib.elmo_int8_matmul.restype = _I
 _lib.elmo_int8_matmul.argtypes = [_P, _L, _P, _P, _L, _P, _P, _L, _L, _L, _P, _L, _I, _P]
+_lib.elmo_int8_matmul_tile.restype = _I
+_lib.elmo_int8_matmul_tile.argtypes = [_L, _L, _L]
 _lib.elmo_sample_bytes.restype = _Z
 _lib.elmo_sample_bytes.argtypes = [_L, _L]
 _lib.elmo_sample.restype = _I
@@ -107,7 +109,8 @@ EXPORTS = ("elmo_last_error", "elmo_logit_buffer_bytes", "elmo_head_sizes", "elm
            "elmo_head_step", "elmo_head_topk", "elmo_head_destroy", "elmo_quantize", "elmo_philox4x32_10",
            "elmo_head_profile", "elmo_head_profile_read", "elmo_precision_hits", "elmo_quantize_em",
            "elmo_dropout_keep16", "elmo_kahan_adamw", "elmo_topk_static", "elmo_rms_norm",
-           "elmo_rms_norm_backward_bytes", "elmo_rms_norm_backward", "elmo_int8_matmul", "elmo_sample_bytes", "elmo_sample",
+           "elmo_rms_norm_backward_bytes", "elmo_rms_norm_backward", "elmo_int8_matmul", "elmo_int8_matmul_tile",
+           "elmo_sample_bytes", "elmo_sample",
            "elmo_distill_bytes", "elmo_distill")
 
 
@@ -342,6 +345,14 @@ def elmo_int8_matmul(a, a_scale, b, b_scale, out, bias=None, *, stream=None) -> 
     pb, _ = _vector("b_scale", b_scale, _ONLY_FP32, N)
     pc, _ = _vector("bias", bias, _ONLY_FP32, N)
     _call(_lib.elmo_int8_matmul, (ap, as_, pa, bp, bs, pb, pc, M, N, K, op, os_, ot), (a, a_scale, b, b_scale, out, bias), stream)
+
+
+def elmo_int8_matmul_tile(M, N, K) -> int:
+    """How a product of these sizes is worked on: tiles of 64, 128 or 256 outputs each way, 0: the kernel of few tokens that streams the weights."""
+    t = int(_lib.elmo_int8_matmul_tile(M, N, K))
+    if t < 0:
+        _check(t)
+    return t
 
 
 def elmo_sample_bytes(rows, V) -> int:

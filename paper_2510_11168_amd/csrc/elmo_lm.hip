@@ -39,8 +39,9 @@ int check_aligned(const char* what, const void* p, int dtype) {
   return 0;
 }
 // Work-items of a launch are counted in 32 bits.
+constexpr bool fits(int64_t workgroups, int threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
 int check_grid(const char* what, int64_t workgroups, int threads) {
-  if (workgroups > (int64_t)UINT32_MAX / threads) return fail(-1, "%s: more rows than one launch takes", what);
+  if (!fits(workgroups, threads)) return fail(-1, "%s: more rows than one launch takes", what);
   return 0;
 }
 // Opt in to more than 64 KiB of LDS, once for each kernel and device, whichever host thread comes first.
@@ -204,30 +205,44 @@ template <class O, int FM> int launch_int8_skinny(const elmo::Int8Args& p, hipSt
 //  - else tiles, by the time of the rounds in which they go over the 256 CUs at K = 4096: 256 x 256 63 a round of 256, 128 x 128 40 a round of 512 (two a
 //    CU; 26 if there are only 256), 64 x 64 18 a round of 512 (14).  8192 x 14336: 406 in tiles of 256, 502 of 128; 2048 x 4096: 50 / 41;
 //    512 x 4096: 42 / 22.5 / 18.8.
+//  - of these only what one launch takes: M and N go up to 2^30, which smaller tiles are too many for (and more than 2^27 outputs a token the streaming kernel).
+int64_t int8_tiles(int64_t M, int64_t N, int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
+int int8_tile_of(int64_t M, int64_t N, int64_t K) {        // 0: the streaming kernel
+  const auto rounds = [](int64_t n, int64_t slots) { return (n + slots - 1) / slots; };
+  if (((M <= 16 && (K >= 2048 || N <= 16384)) || (M <= 32 && N <= 4096)) && fits((N + 15) / 16, elmo::kSkinnyThreads)) return 0;
+  const int64_t n256 = int8_tiles(M, N, 256), n128 = int8_tiles(M, N, 128), n64 = int8_tiles(M, N, 64);
+  const int64_t t256 = 63 * rounds(n256, 256), t128 = !fits(n128, elmo::int8_threads<128, 128, 1, 2>()) ? INT64_MAX : n128 <= 256 ? 26 : 40 * rounds(n128, 512),
+                t64 = !fits(n64, elmo::int8_threads<64, 64, 1, 1>()) ? INT64_MAX : n64 <= 256 ? 14 : 18 * rounds(n64, 512);
+  return t256 <= t128 && t256 <= t64 ? 256 : t128 <= t64 ? 128 : 64;
+}
 template <class O> int launch_int8(elmo::Int8Args p, hipStream_t st) {
   if (p.M == 1) p.as = 0;                                  // (a single row's stride means nothing)
   if (p.N == 1) p.bs = 0;
-  const auto tiles = [&](int t) { return (int64_t)((p.M + t - 1) / t) * ((p.N + t - 1) / t); };
-  const auto rounds = [](int64_t n, int64_t slots) { return (n + slots - 1) / slots; };
-  if (p.M <= 16 && (p.K >= 2048 || p.N <= 16384)) return launch_int8_skinny<O, 1>(p, st);
-  if (p.M <= 32 && p.N <= 4096) return launch_int8_skinny<O, 2>(p, st);
   // (row offsets within a tile are formed from 24-bit factors)
   const bool aligned = !(((uintptr_t)p.a | (uintptr_t)p.b | (uint64_t)p.as | (uint64_t)p.bs) & 15) && p.as < (1 << 24) && p.bs < (1 << 24);
-  const int64_t t256 = 63 * rounds(tiles(256), 256), t128 = tiles(128) <= 256 ? 26 : 40 * rounds(tiles(128), 512),
-                t64 = tiles(64) <= 256 ? 14 : 18 * rounds(tiles(64), 512);
-  if (t256 <= t128 && t256 <= t64) return launch_int8_tiles<O, 256, 256, 2, 4, 2>(p, aligned, st);
-  if (t128 <= t64) return launch_int8_tiles<O, 128, 128, 1, 2, 2>(p, aligned, st);
-  return launch_int8_tiles<O, 64, 64, 1, 1, 4>(p, aligned, st);
+  switch (int8_tile_of(p.M, p.N, p.K)) {
+    case 0: return p.M <= 16 ? launch_int8_skinny<O, 1>(p, st) : launch_int8_skinny<O, 2>(p, st);
+    case 256: return launch_int8_tiles<O, 256, 256, 2, 4, 2>(p, aligned, st);
+    case 128: return launch_int8_tiles<O, 128, 128, 1, 2, 2>(p, aligned, st);
+    default: return launch_int8_tiles<O, 64, 64, 1, 1, 4>(p, aligned, st);
+  }
 }
+constexpr int64_t kInt8Most = (int64_t)1 << 30, kInt8MostK = 131071;      // 131071 products of 128 x 128 stay below 2^31
 }  // namespace
+
+extern "C" int elmo_int8_matmul_tile(int64_t M, int64_t N, int64_t K) {
+  if (M < 1 || M > kInt8Most || N < 1 || N > kInt8Most || K < 0 || K > kInt8MostK) return fail(-1, "M and N must be in [1, 2^30], K in [0, %lld]", (long long)kInt8MostK);
+  const int t = int8_tile_of(M, N, K);
+  if (t == 256) ELMO_TRY(check_grid("elmo_int8_matmul", int8_tiles(M, N, 256), elmo::int8_threads<256, 256, 2, 4>()));
+  return t;
+}
 
 extern "C" int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, const int8_t* b, int64_t b_stride, const float* b_scale,
                                 const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t out_stride, int out_dtype,
                                 void* hip_stream) {
-  constexpr int64_t most = (int64_t)1 << 30, most_k = 131071;      // 131071 products of 128 x 128 stay below 2^31
   if (!is_real(out_dtype)) return fail(-2, "out_dtype must be ELMO_BF16 or ELMO_FP32 (got %d)", out_dtype);
-  if (M < 0 || M > most || N < 0 || N > most) return fail(-1, "M = %lld and N = %lld must be in [0, 2^30]", (long long)M, (long long)N);
-  if (K < 0 || K > most_k) return fail(-1, "K = %lld outside [0, %lld]: longer sums do not fit 32 bits", (long long)K, (long long)most_k);
+  if (M < 0 || M > kInt8Most || N < 0 || N > kInt8Most) return fail(-1, "M = %lld and N = %lld must be in [0, 2^30]", (long long)M, (long long)N);
+  if (K < 0 || K > kInt8MostK) return fail(-1, "K = %lld outside [0, %lld]: longer sums do not fit 32 bits", (long long)K, (long long)kInt8MostK);
   if (M == 0 || N == 0) return 0;
   if ((K > 0 && (!a || !b)) || !a_scale || !b_scale || !out) return fail(-1, "a, b, a_scale, b_scale and out must not be NULL");
   ELMO_TRY(check_stride("a_stride", a_stride, K, M));

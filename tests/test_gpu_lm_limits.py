@@ -104,6 +104,23 @@ def test_norm_backward_of_zeros_and_a_very_small_eps(b):
     assert not dw.any()
 
 
+# ------------------------------------------------------------------ integer product
+def test_int8_matmul_of_more_outputs_than_the_streaming_kernel_takes(b):
+    """2^27 weight rows and some: more than a launch of the kernel of few tokens has workgroups for, and operand offsets beyond 2^31."""
+    M, N, K = 2, (1 << 27) + 5, 16
+    assert b.elmo_int8_matmul_tile(M, N, 2048) == 64 and b.elmo_int8_matmul_tile(M, (1 << 27) - 16, 2048) == 0
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    a, w = torch.randint(-128, 128, (M, K), device=DEV, generator=g, dtype=torch.int8), torch.randint(-128, 128, (N, K), device=DEV, generator=g, dtype=torch.int8)
+    sa, sb = torch.rand(M, device=DEV, generator=g), torch.rand(N, device=DEV, generator=g)
+    y = torch.empty((M, N), device=DEV)
+    b.elmo_int8_matmul(a, sa, w, sb, y)
+    for at in range(0, N, 1 << 24):
+        part = w[at:at + (1 << 24)].float()                      # (sums below 2^24: exact)
+        for m in range(M):
+            assert torch.equal(y[m, at:at + (1 << 24)], (part * a[m].float()).sum(1) * sa[m] * sb[at:at + (1 << 24)])
+
+
 # ------------------------------------------------------------------ sampling
 def draw(b, z, u, **kw):
     token, prob = torch.full((len(u),), -7, dtype=torch.int32, device=DEV), torch.full((len(u),), -7.0, device=DEV)
