@@ -105,6 +105,39 @@ def test_norm_backward_of_zeros_and_a_very_small_eps(b):
 
 
 # ------------------------------------------------------------------ integer product
+def rows_of(t, pad, first=0):
+    """The same values as rows of a wider buffer that begins `first` elements behind an aligned address; what is between rows is 72."""
+    n, d = t.shape
+    wide = torch.full((first + n * (d + pad),), 72, dtype=t.dtype, device=t.device)
+    v = wide[first:].view(n, d + pad)[:, :d]
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("tile,M,N,K", [(64, 300, 700, 200), (128, 1500, 1531, 272), (128, 2050, 2060, 130), (128, 1500, 1531, 100), (256, 3001, 3333, 200), (256, 4090, 4090, 130),
+                                        (256, 3001, 3333, 100), (256, 3071, 3329, 512)])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+def test_int8_matmul_in_each_tile(b, tile, M, N, K, out):
+    """Ragged rows, columns and K, operands whose rows are 16-byte aligned and not, with and without a bias, in the tile that the rule picks."""
+    assert b.elmo_int8_matmul_tile(M, N, K) == tile
+    g = gen(M + K)
+    a, w = (torch.randint(-128, 128, (n, K), generator=g).to(torch.int8) for n in (M, N))
+    a[0], w[0], a[M - 1], w[N - 1] = -128, -128, -128, 127       # the largest sums there are
+    sa, sb, bias = torch.rand(M, generator=g) + 0.1, torch.rand(N, generator=g) * 1e-3, torch.randn(N, generator=g)
+    plain = (f64(a) @ f64(w).T) * f64(sa)[:, None] * f64(sb)[None, :]     # (whole numbers below 2^53)
+    up = -K % 16
+    for pad, first, pad_out, with_bias in ((up, 0, 0, False), (up + 16, 16, 1, True), (5 if up != 5 else 7, 3, 3, True)):
+        y = rows_of(torch.zeros((M, N), dtype=out, device=DEV), pad_out, first)
+        ad, wd = rows_of(a.to(DEV), pad, first), rows_of(w.to(DEV), pad, first)
+        assert (first == 3) == bool((ad.data_ptr() | ad.stride(0)) & 15)
+        b.elmo_int8_matmul(ad, sa.to(DEV), wd, sb.to(DEV), y, bias=bias.to(DEV) if with_bias else None)
+        want = plain + f64(bias) if with_bias else plain
+        # sum to FP32, two products, the bias's addition
+        close(y, want, 3.01 * E * np.abs(plain) + (HALF[out] + 1.01 * E) * np.abs(want) + 1e-38, f"out, pad {pad}")
+        if pad_out:
+            assert bool((torch.as_strided(y, (M - 1, pad_out), (N + pad_out, 1), y.storage_offset() + N) == 72).all()), "nothing between the rows is written"
+
+
 def test_int8_matmul_of_more_outputs_than_the_streaming_kernel_takes(b):
     """2^27 weight rows and some: more than a launch of the kernel of few tokens has workgroups for, and operand offsets beyond 2^31."""
     M, N, K = 2, (1 << 27) + 5, 16
