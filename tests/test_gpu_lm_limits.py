@@ -212,3 +212,128 @@ def test_borders_between_two_tokens(b):
                 first = 0 if order is rows else 1
                 wrong = np.flatnonzero(token.numpy() - first != np.array(want))
                 assert not len(wrong), (dtype, list(kw), len(wrong), "of", len(want))
+
+
+# ------------------------------------------------------------------ workspaces, graphs, streams
+def split_state(seed):
+    """Sampling without top-k of few long rows, by several workgroups a row, in both types; distillation of few long rows; a norm's backward pass."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    rn = lambda *s: torch.randn(s, device=DEV, generator=g)  # noqa: E731
+    bf, rows = torch.bfloat16, 6
+    s = dict(z16=(2.5 * rn(rows, 70001)).to(bf), z32=2.5 * rn(rows, 20011), u=torch.rand(rows, device=DEV, generator=g), t=0.5 + torch.rand(rows, device=DEV, generator=g),
+             p=torch.rand(rows, device=DEV, generator=g), m=0.02 * torch.rand(rows, device=DEV, generator=g),
+             ti=torch.randint(0, 70001, (rows, 30), device=DEV, generator=g, dtype=torch.int32), tz=rn(rows, 30), dy=rn(70, 900), h=rn(70, 900), w=1 + 0.1 * rn(900))
+    s["p"][:2] = torch.tensor([1.0, 0.0])                        # off; one token
+    s["t"][2] = 0.0                                              # greedy
+    s["z32"][3] = 1.0                                            # a bin that overflows the list
+    s["z16"][4] *= 1e-6
+    for k, n, t in (("k16", (rows,), torch.int32), ("k32", (rows,), torch.int32), ("q16", (rows,), torch.float32), ("q32", (rows,), torch.float32), ("loss", (rows,), torch.float32),
+                    ("dz", (rows, 70001), bf), ("dh", (70, 900), torch.float32), ("dw", (900,), torch.float32)):
+        s[k] = torch.zeros(n, dtype=t, device=DEV)
+    return s
+
+
+SPLIT_OUTPUTS = ("k16", "q16", "k32", "q32", "loss", "dz", "dh", "dw")
+
+
+def split_calls(b, s, stream=None, ws=None):
+    w = (lambda n: ws[:n]) if ws is not None else (lambda n: None)
+    b.elmo_sample(s["z16"], s["u"], s["k16"], temperature=s["t"], top_p=s["p"], min_p=s["m"], prob_out=s["q16"], stream=stream, workspace=w(b.elmo_sample_bytes(*s["z16"].shape)))
+    b.elmo_sample(s["z32"], s["u"], s["k32"], temperature=s["t"], top_p=s["p"], prob_out=s["q32"], stream=stream, workspace=w(b.elmo_sample_bytes(*s["z32"].shape)))
+    b.elmo_distill(s["z16"], s["ti"], s["tz"], s["loss"], s["dz"], temperature=1.5, stream=stream, workspace=w(b.elmo_distill_bytes(*s["z16"].shape)))
+    b.elmo_rms_norm_backward(s["dy"], s["h"], s["dh"], s["w"], 1e-6, dweight=s["dw"], stream=stream, workspace=w(b.elmo_rms_norm_backward_bytes(*s["h"].shape)))
+
+
+def test_split_rows_give_the_oracles_tokens(b):
+    from test_gpu_lm import check_tokens
+    s = split_state(3)
+    split_calls(b, s)
+    get = {k: s[k].cpu() for k in ("t", "p", "m", "u")}
+    check_tokens(s["z16"].cpu(), get["u"], s["k16"].cpu(), s["q16"].cpu(), t=get["t"], top_p=get["p"], min_p=get["m"])
+    check_tokens(s["z32"].cpu(), get["u"], s["k32"].cpu(), s["q32"].cpu(), t=get["t"], top_p=get["p"])
+
+
+@pytest.mark.parametrize("own", [False, True])
+def test_split_rows_captured_and_replayed(b, own):
+    """A captured run replays to the eager run's bits on new inputs, with eager work between the replays; with a workspace of the caller's, all calls of the run one after another
+    in the same one."""
+    s, side = split_state(1), torch.cuda.Stream()
+    ws = torch.full((1 << 21,), 255, dtype=torch.uint8, device=DEV) if own else None
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        split_calls(b, s, ws=ws)                                 # kernels loaded before the capture
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        split_calls(b, s, ws=ws)
+    for seed in (2, 3, 4):
+        new = split_state(seed)
+        for k in s:
+            s[k].copy_(new[k])
+        graph.replay()
+        torch.cuda.synchronize()
+        split_calls(b, new)
+        torch.cuda.synchronize()
+        for k in SPLIT_OUTPUTS:
+            assert torch.equal(s[k], new[k]), (seed, k)
+
+
+def test_split_rows_on_two_streams_at_once(b):
+    states = [split_state(s) for s in (5, 6)]
+    alone = []
+    for s in states:
+        split_calls(b, s)
+        torch.cuda.synchronize()
+        alone.append({k: s[k].clone() for k in SPLIT_OUTPUTS})
+        for k in SPLIT_OUTPUTS:
+            s[k].zero_()
+    streams = [torch.cuda.Stream() for _ in states]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, stream in zip(states, streams):
+            split_calls(b, s, stream=stream)
+    torch.cuda.synchronize()
+    for s, want in zip(states, alone):
+        for k in SPLIT_OUTPUTS:
+            assert torch.equal(s[k], want[k]), k
+
+
+def test_one_workspace_for_calls_that_follow_one_another(b):
+    """Of exactly the stated size, full of ones at first and of the call before's leavings then, with guards behind it: the bits of calls with fresh workspaces."""
+    g = gen(12)
+    ws = torch.full((16 << 20,), 255, dtype=torch.uint8, device=DEV)
+
+    def exact(n):
+        ws[n:].fill_(255)
+        return ws[:n]
+
+    def guarded(n):
+        assert bool((ws[n:] == 255).all()), "nothing behind the workspace is written"
+    for i, (rows, V, dtype) in enumerate([(6, 70001, torch.bfloat16), (40, 16384, torch.float32), (1, 131072, torch.bfloat16), (3, 30000, torch.float32), (6, 70001, torch.bfloat16),
+                                          (128, 16400, torch.float32), (2, 200003, torch.bfloat16), (3, 200003, torch.float32)]):
+        z, u = (2.5 * torch.randn((rows, V), generator=g)).to(dtype).to(DEV), torch.rand(rows, generator=g).to(DEV)
+        p = None if i % 3 == 2 else torch.rand(rows, generator=g).to(DEV)
+        n = b.elmo_sample_bytes(rows, V)
+        assert n > 0
+        token, prob = (torch.empty(rows, dtype=t, device=DEV) for t in (torch.int32, torch.float32))
+        fresh, fresh_prob = torch.empty_like(token), torch.empty_like(prob)
+        b.elmo_sample(z, u, token, top_p=p, prob_out=prob, workspace=exact(n))
+        guarded(n)
+        b.elmo_sample(z, u, fresh, top_p=p, prob_out=fresh_prob)
+        assert torch.equal(token, fresh) and torch.equal(prob, fresh_prob), (rows, V)
+        ti, tz = torch.randint(0, V, (rows, 9), generator=g, dtype=torch.int32).to(DEV), torch.randn((rows, 9), generator=g).to(DEV)
+        n = b.elmo_distill_bytes(rows, V)
+        loss, again, grad, grad2 = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty_like(z), torch.empty_like(z)
+        b.elmo_distill(z, ti, tz, loss, grad, workspace=exact(n))
+        guarded(n)
+        b.elmo_distill(z, ti, tz, again, grad2)
+        assert torch.equal(loss, again) and torch.equal(grad, grad2), (rows, V)
+        d = 100 + 37 * i
+        h, dy = torch.randn((rows, d), generator=g).to(DEV), torch.randn((rows, d), generator=g).to(DEV)
+        n = b.elmo_rms_norm_backward_bytes(rows, d)
+        dh, dw, dw2 = torch.empty_like(h), torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+        b.elmo_rms_norm_backward(dy, h, dh, None, 1e-6, dweight=dw, workspace=exact(n))
+        guarded(n)
+        b.elmo_rms_norm_backward(dy, h, dh, None, 1e-6, dweight=dw2)
+        assert torch.equal(dw, dw2)
