@@ -337,3 +337,57 @@ def test_one_workspace_for_calls_that_follow_one_another(b):
         guarded(n)
         b.elmo_rms_norm_backward(dy, h, dh, None, 1e-6, dweight=dw2)
         assert torch.equal(dw, dw2)
+
+
+# ------------------------------------------------------------------ distillation
+def records(z):
+    """How often a thread's maximum moves at most, wherever the stretch of rounds begins that it takes: octet i of a row is thread i % 512's."""
+    rows, V = z.shape
+    n = -(-V // 4096)
+    top = np.full((rows, n * 512), -np.inf)
+    whole = z[:, :V // 8 * 8].reshape(rows, -1, 8)
+    top[:, :whole.shape[1]] = whole.max(axis=2)
+    top, most = top.reshape(rows, n, 512), 0
+    for start in range(n):
+        m = np.maximum.accumulate(top[:, start:], axis=1)
+        most = max(most, int((np.diff(m, axis=1) > 0).sum(axis=1).max(initial=0)))
+    return most
+
+
+def distill_tolerances(z, idx, T, v, dtype, want):
+    """The student's sum: v_exp_f32 (2 e) for a token, for each step of its thread's maximum, and for the steps to the wave's, the workgroup's and the row's; arguments, whose
+    difference, constant and product are rounded: 3 e of (max - z) / T over all the steps together; three additions in an octet (3 e); above octets FP64.  The
+    loss takes that sum's logarithm and FP64 terms and is rounded once.  The gradient: p with one exponential (2 e and 3 e of the argument), the sum's
+    rounding, v T, quotient, product (5 e); q v T with three roundings and an addition; the difference's."""
+    Z = f64(z) / T
+    fin = np.where(np.isfinite(Z), Z, -np.inf)
+    top = fin.max(axis=1, keepdims=True)
+    x = np.where(np.isfinite(fin), top - fin, 0.0)
+    p = np.exp(fin - top)
+    p = p / p.sum(axis=1, keepdims=True)
+    vv = np.ones((len(Z), 1)) if v is None else f64(v)[:, None]
+    dS = E * (2 * (1 + records(fin) + 3) + 3 + 3 * np.sum(p * x, axis=1, keepdims=True))
+    loss, grad = want
+    tl = np.abs(vv[:, 0]) * T * T * (dS[:, 0] + 2.0 ** -48 * (np.max(x, axis=1) + 20)) + 1.01 * E * np.abs(loss) + 1e-38
+    q = np.abs(grad / np.where(vv == 0, 1, vv) / T - p)
+    tg = np.abs(vv) * T * (p * (dS + E * (2 + 3 * x + 5)) + 4 * E * q) + (HALF[dtype] + 2 * E) * np.abs(grad) + 1e-38
+    return tl, tg
+
+
+@pytest.mark.parametrize("rows,V,K,T", [(2, 300, 40, 1.0), (3, 32003, 1000, 1.0), (2, 131072, 1024, 2.0), (200, 20011, 512, 0.75), (1, 300007, 1024, 1.0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_distill_of_a_student_that_agrees(b, rows, V, K, T, dtype):
+    """The teacher's tokens hold practically all of the mass, with the student's logits but for 3e-2: the loss is a small difference of large terms."""
+    g = gen(V + K)
+    z = 2 * torch.randn((rows, V), generator=g) - 25 * T
+    idx = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(rows)]).to(torch.int32)
+    heads = 2 * torch.randn((rows, K), generator=g)
+    z = z.scatter(1, idx.long(), heads).to(dtype)
+    tz = z.gather(1, idx.long()).float() + 3e-2 * torch.randn((rows, K), generator=g)
+    loss, grad = torch.empty(rows, device=DEV), torch.empty((rows, V), dtype=dtype, device=DEV)
+    b.elmo_distill(z.to(DEV), idx.to(DEV), tz.to(DEV), loss, grad, temperature=T)
+    want = o.distill(f64(z), idx.numpy(), f64(tz), T)
+    assert np.all(want[0] < 5e-3)
+    tl, tg = distill_tolerances(z, idx, T, None, dtype, want)
+    close(loss, want[0], tl, "loss")
+    close(grad, want[1], tg, "gradient")
