@@ -391,3 +391,29 @@ def test_distill_of_a_student_that_agrees(b, rows, V, K, T, dtype):
     tl, tg = distill_tolerances(z, idx, T, None, dtype, want)
     close(loss, want[0], tl, "loss")
     close(grad, want[1], tg, "gradient")
+
+
+# ------------------------------------------------------------------ long rows
+@pytest.mark.parametrize("V", [2_200_003, 3_000_001])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_millions_of_outputs(b, V, dtype):
+    """Segments of several rounds (above 2097152 tokens), split and by one workgroup; distillation of such rows."""
+    from test_gpu_lm import check_tokens
+    g, rows = gen(V), 3
+    z = (2.5 * torch.randn((rows, V), generator=g)).to(dtype)
+    z[1, ::3] = -float("inf")
+    z[2] = z[2].round()                                          # ties of hundreds of thousands
+    for kw in (dict(), dict(top_p=0.9), dict(top_p=0.4, min_p=0.001, t=0.8), dict(top_k=50), dict(top_k=5000, top_p=0.9), dict(t=0.0), dict(top_k=2 ** 31 - 1)):
+        u = torch.rand(rows, generator=g)
+        s = {n: torch.full((rows,), v, dtype=torch.int32 if n == "top_k" else torch.float32) for n, v in kw.items()}
+        token, prob = draw(b, z, u, **{"temperature" if n == "t" else n: v for n, v in s.items()})
+        check_tokens(z, u, token, prob, **s)
+    idx, tz = torch.randint(0, V, (rows, 20), generator=g, dtype=torch.int32), torch.randn((rows, 20), generator=g)
+    loss, grad = torch.empty(rows, device=DEV), torch.empty((rows, V), dtype=dtype, device=DEV)
+    b.elmo_distill(z.to(DEV), idx.to(DEV), tz.to(DEV), loss, grad)
+    want = o.distill(f64(z), idx.numpy(), f64(tz), 1.0)
+    tl, tg = distill_tolerances(z, idx, 1.0, None, dtype, want)
+    some = np.isfinite(want[0])                                  # (a masked token of the teacher's: infinite, by definition)
+    assert np.all(np.isposinf(f64(loss)[~some]))
+    close(loss[torch.from_numpy(some)], want[0][some], tl[some], "loss")
+    close(grad, want[1], tg, "gradient")
