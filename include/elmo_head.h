@@ -218,13 +218,13 @@ void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t o
  *    elements from one row to the next, at least the row's length (any value for a single row).
  *    Rows need no alignment beyond their elements'.  Nothing between rows is written.
  *  - Values are ELMO_BF16 or ELMO_FP32 as the dtype argument says; sums are FP32 or wider, every
- *    output is rounded once, to nearest even (overflow to infinity, NaN kept).
+ *    output is rounded once, to nearest even (overflow to infinity, NaN kept); E4M3 rows by way of FP32.
  *  - All pointers are device pointers owned by the caller.  A call with no rows is a no-op.  Workspaces are scratch of the call: two calls that may
  *    overlap in time (streams, captured graphs) need one each.
  *  - Only kernels are enqueued, so after one ordinary call of its kind a call can be captured into
  *    a HIP graph.  The same call gives the same bits every time.
- *  - A launch takes less than 2^32 work-items: 2^22 rows of elmo_sample, 2^23 of elmo_distill, 2^24 of
- *    elmo_rms_norm (2^26 of at most 1024 columns); more are refused.
+ *  - A launch takes fewer than 2^32 work-items: fewer than 2^22 rows of elmo_sample and 2^23 of elmo_distill; of
+ *    elmo_rms_norm fewer than 2^24, of more than 8192 columns 2^22, of at most 1024 columns at most 2^26 - 4.  More are refused.
  * --------------------------------------------------------------------------------------------- */
 
 /* Root-mean-square norm of rows of d elements (1 <= d <= 16384), behind a residual's addition:
@@ -233,8 +233,9 @@ void elmo_philox4x32_10(const uint32_t ctr[4], const uint32_t key[2], uint32_t o
  * receives h rounded to dtype, y is formed from the unrounded h.  y_dtype: ELMO_BF16 or ELMO_FP32, or 8 bits
  * with a scale per row in scale_out [rows]: with p = weight * h and m = max |p| of the row
  *   ELMO_INT8:      y = round(127 p / m),       scale = m / (127 sqrt(mean(h^2) + eps))
- *   ELMO_FP8_E4M3:  y = round_E4M3(448 p / m),  scale = m / (448 sqrt(mean(h^2) + eps))
- * so that y * scale is the norm; the quotient is p * (127 * (1 / m)), p exact and three FP64 roundings.  A row of zeros gives zeros and scale 0; a row that holds an infinity or NaN, or whose squares
+ *   ELMO_FP8_E4M3:  y = round_E4M3(round_FP32(448 p / m)),  scale = m / (448 sqrt(mean(h^2) + eps))
+ * so that y * scale is the norm; the quotient is p * (127 * (1 / m)), p exact and three FP64 roundings.  The conversion to E4M3 takes FP32 values: an
+ * element is off by at most half a step and 2^-24 of its value (one in some million has its other neighbour by that).  A row of zeros gives zeros and scale 0; a row that holds an infinity or NaN, or whose squares
  * add up to more than FP32 holds, gives zeros and scale NaN (BF16 and FP32 rows of such squares are normalised as any others).  sum_out may be x or residual, and y the other of the two, where address, stride and dtype are the same. */
 int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int64_t d, const void* residual,
                   int64_t residual_stride, const void* weight, int weight_dtype, float eps, void* sum_out,
@@ -254,7 +255,7 @@ int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int
 /* 8-bit integer product with a scale for each row of either operand (token and output channel):
  *   out[m, n] = (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]
  * a [M, K] and b [N, K] int8 (all 256 values), scales and bias FP32 (bias NULL = none), out [M, N] in out_dtype.  The sum is exact
- * (0 <= K <= 131071; of no products it is 0).  M and N up to 2^30, fewer than 2^23 tiles of 256 x 256 outputs.
+ * (0 <= K <= 131071; of no products it is 0) and rounded to FP32, as are the two products and the bias's addition.  M and N up to 2^30, fewer than 2^23 tiles of 256 x 256 outputs.
  * elmo_int8_matmul_tile: how these sizes are worked on, in tiles of 64, 128 or 256, or 0 for the kernel of few tokens that streams the weights (-1: refused). */
 int elmo_int8_matmul(const int8_t* a, int64_t a_stride, const float* a_scale, const int8_t* b, int64_t b_stride,
                      const float* b_scale, const float* bias, int64_t M, int64_t N, int64_t K, void* out,
