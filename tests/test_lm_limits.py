@@ -37,3 +37,14 @@ def test_int8_tiles_of_known_sizes(b):
     for M, N, K, tile in ((1, 4096, 4096, 0), (16, 8192, 8192, 0), (16, 131072, 768, 64), (32, 4096, 4096, 0), (33, 4096, 4096, 64), (37, 32003, 4096, 64), (512, 4096, 4096, 64),
                           (2048, 4096, 4096, 128), (8192, 14336, 4096, 256)):
         assert b.elmo_int8_matmul_tile(M, N, K) == tile, (M, N, K)
+
+
+def test_more_rows_than_a_launch_takes_are_refused(b):
+    """At the first number that the header excludes.  The addresses are never read: every call ends in the host's checks."""
+    P = 4096
+    norm = lambda rows, d: b._lib.elmo_rms_norm(P, d, b.ELMO_BF16, rows, d, None, 0, None, 0, 1e-6, None, 0, P, d, b.ELMO_BF16, None, None)  # noqa: E731
+    assert norm(1 << 24, 2048) == -1 and norm(1 << 24, 8192) == -1 and norm(1 << 22, 8193) == -1 and norm(1 << 22, 16384) == -1
+    assert norm((1 << 26) - 3, 1024) == -1 and norm((1 << 26) - 3, 1) == -1
+    assert b._lib.elmo_sample(P, 8, b.ELMO_BF16, 1 << 22, 8, P, None, None, None, None, P, None, None, 0, None) == -1
+    assert b._lib.elmo_distill(P, 8, b.ELMO_BF16, 1 << 23, 8, P, P, b.ELMO_FP32, 1, 1.0, None, P, None, 0, None, 0, None) == -1
+    assert "launch" in b.elmo_last_error()
