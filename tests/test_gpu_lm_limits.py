@@ -417,3 +417,44 @@ def test_millions_of_outputs(b, V, dtype):
     assert np.all(np.isposinf(f64(loss)[~some]))
     close(loss[torch.from_numpy(some)], want[0][some], tl[some], "loss")
     close(grad, want[1], tg, "gradient")
+
+
+# ------------------------------------------------------------------ beside a head
+def test_a_heads_inputs_scores_and_input_gradient(b):
+    """The norm's rows are a head's inputs, its top scores the logits to sample from and the teacher of a smaller student, its input gradient what the norm's backward pass takes."""
+    from test_gpu_lm import check_tokens
+    rows, d, L, k, bf = 24, 256, 5003, 40, torch.bfloat16
+    g = gen(21)
+    x, r, w = torch.randn((rows, d), generator=g).to(bf).to(DEV), torch.randn((rows, d), generator=g).to(bf).to(DEV), (1 + 0.1 * torch.randn(d, generator=g)).to(DEV)
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    b.elmo_rms_norm(x, y, w, 1e-6, residual=r, sum_out=h)
+    head = b.Head(L, d, b.ELMO_BF16, 1024, b.ELMO_SR, rows, 4 * rows)
+    head.weights().copy_((0.2 * torch.randn((L, d), generator=g)).to(bf).to(DEV).view(torch.int16))
+    idx, score = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV)
+    head.topk(y, k, idx, score)
+
+    u, t, p = torch.rand(rows, generator=g), torch.full((rows,), 0.8), torch.full((rows,), 0.9)
+    place, prob = draw(b, score, u, temperature=t, top_p=p)
+    check_tokens(score.cpu(), u, place, prob, t=t, top_p=p)
+    label = idx.gather(1, place.long()[:, None].to(DEV))
+    assert bool(((label >= 0) & (label < L)).all())
+
+    z = torch.randn((rows, L), generator=g).to(bf)
+    loss, dz = torch.empty(rows, device=DEV), torch.empty((rows, L), dtype=bf, device=DEV)
+    b.elmo_distill(z.to(DEV), idx, score, loss, dz, temperature=2.0)
+    want = o.distill(f64(z), idx.cpu().numpy(), f64(score), 2.0)
+    tl, tg = distill_tolerances(z, idx.cpu(), 2.0, None, bf, want)
+    close(loss, want[0], tl, "loss")
+    close(dz, want[1], tg, "gradient")
+
+    labels = torch.stack([torch.randperm(L, generator=g)[:3].sort().values for _ in range(rows)]).to(torch.int32)
+    indptr = torch.arange(0, 3 * rows + 1, 3, dtype=torch.int32, device=DEV)
+    dy, dh, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(d, device=DEV)
+    head.step(y, indptr, labels.flatten().to(DEV), 0.01, 1, 1, dX_out=dy)
+    b.elmo_rms_norm_backward(dy, h, dh, w, 1e-6, dweight=dw)
+    assert bool(dy.float().abs().max() > 0)
+    want, wantw = o.rms_norm_backward(f64(dy), f64(h), f64(w), 1e-6)
+    th, tw = back_tolerances(dy.cpu(), h.cpu(), w.cpu(), 1e-6, bf, want)
+    close(dh, want, th, "dh")
+    close(dw, wantw, tw, "dweight")
+    head.close()
