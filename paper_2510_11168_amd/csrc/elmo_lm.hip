@@ -57,7 +57,8 @@ template <class Kernel> int raise_lds(Kernel* kernel, int bytes, std::once_flag 
 #define ELMO_TRY(call) do { if (int rc_ = (call)) return rc_; } while (0)
 
 // ---- norm: waves of a row and octets of a lane.  Short rows a wave each, without a barrier; longer ones four waves, with as much in flight in fewer
-// registers (16384 rows of 1024 BF16 -> INT8: 24.6 us with one wave, 31.0 with four; of 4096: 104 and 97; 1 row of 4096: 9.1 and 4.4).
+// registers (replayed in a graph, 16384 rows of 1024 BF16 -> INT8: 25.4 us with one wave, 31.4 with four; of 4096: 107 and 95, and 88 on buffers that take turns; 1 row of 4096:
+// 8.8 and 4.1).
 struct RowShape { int wpr, steps; };
 RowShape norm_shape(int d) {
   if (d <= 1024) return {1, (d + 511) / 512};
@@ -89,7 +90,7 @@ template <class T> int launch_norm_out(const elmo::NormArgs& a, int out, hipStre
 }
 
 // Backward: a team of waves keeps its columns' share of the weight gradient over all rows it takes, and a workgroup leaves one share: 512 of them (16384 x
-// 4096 BF16: 103 us; with the shares' sum as it was before 107, 256 of them 136, 1024 of them 127).
+// 4096 BF16, replayed in a graph: 105 us; 256 of them 127, 1024 of them 113).
 constexpr int kNormShares = 512;
 int back_shares(int64_t rows, int64_t d) {
   const int64_t teams = d <= 1024 ? 4 : 1;               // of a workgroup
@@ -261,8 +262,8 @@ namespace {
 constexpr int64_t kMostV = ((int64_t)1 << 31) - 1;
 
 // Workgroups of a row without top-k: one where the rows fill the chip or are short.  Top-p, us, split and (a row more, or an element less) whole.  FP32:
-// 128 rows of 131072 70 and 118, one of 16384 20.9 and 22.5.  BF16, where one workgroup takes a row by codes in about half the time: 32 rows of 131072 36 and
-// 44, of 65536 30 and 28, one row of 65536 22 and 28; one of 32768 22.5 and 20.3; 64 rows of 131072 48 and 44.
+// 128 rows of 131072 71 and 122, one of 16384 21.8 and 23.5.  BF16, where one workgroup takes a row by codes in about half the time: 32 rows of 131072 37 and
+// 44, of 65536 30 and 32, one row of 65536 23 and 28; one of 32768 22.5 and 20.3; 64 rows of 131072 48 and 44.
 constexpr int64_t kSampleSplitRows = 128, kSampleSplitV = 16384, kSampleSplitRowsBf16 = 32, kSampleSplitVBf16 = 65536;
 int sample_parts(int64_t rows, int64_t V, bool bf16) {
   if (rows > (bf16 ? kSampleSplitRowsBf16 : kSampleSplitRows) || V < (bf16 ? kSampleSplitVBf16 : kSampleSplitV)) return 1;
@@ -319,7 +320,7 @@ extern "C" int elmo_sample(const void* logits, int64_t logits_stride, int dtype,
 }
 
 namespace {
-// Workgroups of a row: one where the rows fill the chip or are short, else up to 64, each with at least one round of octets (131072 BF16: 1 row 9 - 11 us,
+// Workgroups of a row: one where the rows fill the chip or are short, else up to 64, each with at least one round of octets (131072 BF16: 1 row 8.7 - 11 us,
 // 128 rows 24.0, 129 rows, a workgroup each, 31.0).
 int distill_parts(int64_t rows, int64_t V) {
   const int64_t rounds = (V / 8 + elmo::kDistillThreads - 1) / elmo::kDistillThreads;

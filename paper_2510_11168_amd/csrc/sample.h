@@ -9,8 +9,8 @@
 // weight over that sum: few bits of a light token's W are left.
 //
 // Bound: a row is read two to four times, by one workgroup, and stays in the caches for the second time on; where many tokens are kept it is the
-// weights' arithmetic (some twenty FP64 and integer instructions each).  BF16 256 x 131072: top-p 54 us, no filter (no counts) 39, greedy (two plain
-// readings) 23.  What is done, by the row's settings:
+// weights' arithmetic (some twenty FP64 and integer instructions each).  256 x 131072 in us, BF16 and FP32: greedy (two plain readings) 23 and 41, top-k
+// 50 with top-p 29 and 44, top-k 2000 53 and 124, top-p 55 and 131, no filter (BF16, no counts) 39.  What is done, by the row's settings:
 //   top_k <= 512   the k-th largest of the threads' maxima bounds the k-th token from below; the few tokens above it go to a list in LDS,
 //                  which is sorted, filtered and drawn from: two readings, no weights but the list's;
 //   top_p, top_k   counts and weights over bins of 1/64 octave of weight, then the tokens of the bin in which the filter ends, sorted (a bin

@@ -26,7 +26,7 @@
 #define __builtin_amdgcn_readfirstlane(x) (x)
 
 namespace emu {
-constexpr int kThreads = 1024, kStack = 256 << 10;
+constexpr int kThreads = 1024, kStack = 64 << 10;
 struct Index { unsigned x; };
 static Index thread, block;
 static int me;                                   // the running thread, -1 outside of one
