@@ -244,7 +244,7 @@ int elmo_rms_norm(const void* x, int64_t x_stride, int dtype, int64_t rows, int6
 /* Its backward pass.  h: what was normalised (sum_out, or x without a residual).  With R = 1 / sqrt(mean(h^2) + eps), g = weight * dy:
  *   dh = R (g - h R^2 mean(g h)) + dsum      (the gradient of x and of the residual alike)
  *   dweight[j] = sum over rows of R dy h     (FP32 [d], overwritten; NULL = not wanted; zeros for no rows)
- * R itself has to lie within FP32.  dsum (NULL = none) is the gradient that reaches sum_out from elsewhere.  dh may be dy, h or dsum where address and stride are
+ * h is taken as it is stored: behind a BF16 sum_out the gradient is that at the rounded sum.  R itself has to lie within FP32.  dsum (NULL = none) is the gradient that reaches sum_out from elsewhere.  dh may be dy, h or dsum where address and stride are
  * the same.  dweight needs a workspace of elmo_rms_norm_backward_bytes(rows, d) bytes, 4-byte aligned. */
 size_t elmo_rms_norm_backward_bytes(int64_t rows, int64_t d);
 int elmo_rms_norm_backward(const void* dy, int64_t dy_stride, const void* h, int64_t h_stride, int dtype, int64_t rows,
