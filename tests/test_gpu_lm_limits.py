@@ -95,6 +95,25 @@ def test_norm_backward_of_large_and_small_rows(b, rows, d, dtype, rms, eps):
     close(dw, wantw, tw, "dweight")
 
 
+@pytest.mark.parametrize("rows,d", [(2500, 300), (1300, 2048), (1100, 9000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_backward_of_rows_of_all_sizes_by_one_team(b, rows, d, dtype):
+    """A team that takes several rows one after another, ordinary ones and ones that are summed twice."""
+    g = gen(rows)
+    size = torch.tensor([1e18, 1.0, 1e-25, 3.0, 1.0, 1e30, 1e-25])[torch.randint(0, 7, (rows,), generator=g)][:, None]
+    h = (size * torch.randn((rows, d), generator=g)).to(dtype)
+    dy = (h.float() / size + 0.1 * torch.randn((rows, d), generator=g)).to(dtype)
+    dh, dw, again = torch.empty((rows, d), dtype=dtype, device=DEV), torch.empty(d, device=DEV), torch.empty(d, device=DEV)
+    args = dy.to(DEV), h.to(DEV), dh, None, 0.0
+    b.elmo_rms_norm_backward(*args, dweight=dw)
+    want, wantw = o.rms_norm_backward(f64(dy), f64(h), np.ones(d), 0.0)
+    th, tw = back_tolerances(dy, h, torch.ones(d), 0.0, dtype, want)
+    close(dh, want, th, "dh")
+    close(dw, wantw, tw, "dweight")
+    b.elmo_rms_norm_backward(*args, dweight=again)
+    assert torch.equal(again, dw)
+
+
 def test_norm_backward_of_zeros_and_a_very_small_eps(b):
     h, dy = torch.zeros((2, 300), device=DEV), torch.randn((2, 300), generator=gen(1)).to(DEV)
     dh, dw = torch.empty_like(h), torch.empty(300, device=DEV)
